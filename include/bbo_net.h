@@ -1,0 +1,148 @@
+/*
+ * bbo_net.h — C ABI of the operators of a wide residual network in 8 bits, for MI355X.
+ *
+ * The evaluator of bbo_mlp.h scores thousands of small models; the model that a search picks is then trained once at
+ * full width and served.  These are the operators of that: the norm of the residual stream, matrices in 8 bits with a
+ * scale for each block of 128, their product, and an AdamW step over all tensors of a model.
+ *
+ * Conventions
+ *   - Pointers are HIP device memory on the current device unless said otherwise; the caller owns every buffer.  The
+ *     library allocates nothing and keeps nothing between calls.  Work is enqueued on the caller's stream (hipStream_t,
+ *     NULL = default stream) and the calls return without waiting; all of them may be captured into a graph.
+ *   - Strides are in elements from one row to the next (bytes for 8-bit matrices and their scales) and at least the
+ *     row's length; rows themselves are dense.  Any alignment of an element's type will do; 8-bit matrices whose rows
+ *     start at multiples of 16 bytes, with scales whose rows start at multiples of 4, are the fast ones.
+ *   - Outputs do not overlap inputs, except where a function says so.
+ *   - Every function returns BBO_OK or an error code of bbo_mlp.h; bbo_net_last_error() has the message of the calling
+ *     thread's last failure.  Nothing throws or aborts.  No rows is a no-op returning BBO_OK.
+ *   - The same call on the same inputs gives the same bits: sums have a fixed order, no atomics.
+ *
+ * 8-bit matrices ("blocks of 128")
+ *   Values are OCP e4m3 bytes, row-major.  A block is 128 columns of one row (tile 1) or of 128 rows (tile 128), the
+ *   last ones shorter.  Its scale is a power of two 2^(byte - 127), byte 0..254 (255: NaN), in
+ *   scales[row / tile][column / 128].  The value stood for is e4m3 * scale.  Scales are powers of two because a
+ *   floating-point code loses nothing by that, and the matrix units apply them at no cost.
+ */
+#ifndef BBO_NET_H
+#define BBO_NET_H
+
+#include <stddef.h>
+#include <stdint.h>
+
+#include "bbo_mlp.h"
+
+#ifdef __cplusplus
+extern "C" {
+#endif
+
+#define BBO_NET_MAX_WIDTH 32768 /* of a normed row */
+
+/* How AdamW's moments are held. */
+enum { BBO_NET_MOMENTS_F32 = 0, BBO_NET_MOMENTS_8BIT = 1 };
+
+/*
+ * h = x + residual; y = h / sqrt(mean(h^2) + eps) * weight, per row.
+ *   x, residual, sum, y   [rows][width] of dtype (BBO_F32 | BBO_BF16); residual may be NULL (h = x)
+ *   weight                float32 [width], or NULL for ones
+ *   sum                   h rounded to dtype: what the norm is then taken of, and what its gradient needs.  NULL without
+ *                         a residual, required with one; may be x or residual itself
+ *   y, rstd, q            outputs, each may be NULL: y in dtype; 1 / sqrt(mean(h^2) + eps) as float32 [rows]; y in 8 bits
+ *                         (tile 1), rounded once from float32, with its scales [rows][ceil(width / 128)]
+ * Sums of squares are in float32: a row whose squares pass 3.4e38 gets y = 0.
+ * Errors: BBO_INVALID_ARG, BBO_UNSUPPORTED (width), BBO_DEVICE_ERROR.
+ */
+int bbo_net_rms_norm(const void* x, int64_t x_stride, const void* residual, int64_t residual_stride, const float* weight,
+                     int64_t rows, int64_t width, float eps, int32_t dtype, void* sum, int64_t sum_stride, void* y,
+                     int64_t y_stride, float* rstd, void* q, int64_t q_stride, void* q_scales, int64_t q_scale_stride,
+                     void* stream);
+
+/* Bytes of workspace for bbo_net_rms_norm_grad with a dweight; writes *out. */
+int bbo_net_rms_norm_grad_workspace(int64_t rows, int64_t width, size_t* out);
+
+/*
+ * The norm's gradient: with xhat = h rstd and g = dy weight,
+ *   dx = rstd (g - xhat mean(g xhat)) + dsum   (the gradient of x and of residual alike)
+ *   dweight = sum over rows of dy xhat
+ *   dy, h, dsum, dx   [rows][width] of dtype; h: the call's x, or its sum where it had a residual; dsum: the gradient that
+ *                     arrives at sum, or NULL; dx may be dy or dsum itself
+ *   rstd, weight      as of the forward call
+ *   dweight           float32 [width], or NULL (then no workspace is needed); written also for no rows (zeros)
+ *   workspace         16-byte aligned, bbo_net_rms_norm_grad_workspace() bytes
+ */
+int bbo_net_rms_norm_grad(const void* dy, int64_t dy_stride, const void* dsum, int64_t dsum_stride, const void* h,
+                          int64_t h_stride, const float* rstd, const float* weight, int64_t rows, int64_t width, int32_t dtype,
+                          void* dx, int64_t dx_stride, float* dweight, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * A matrix into 8 bits, in its own order, transposed, or both from one reading.
+ *   x      [rows][cols] of dtype
+ *   gate   [rows][cols] of dtype, or NULL: a value whose gate is <= 0 counts as 0 (gate = x is ReLU; gate = the
+ *          activation's input with x its gradient is ReLU's gradient).  A NaN gate lets the value through
+ *   tile   1 or 128
+ *   q, scales      [rows][cols], [ceil(rows / tile)][ceil(cols / 128)], or both NULL
+ *   qt, t_scales   the transpose: [cols][rows], [ceil(cols / tile)][ceil(rows / 128)], or both NULL
+ * A block's scale brings its largest finite magnitude into (224, 448]; values are rounded to nearest, ties to even.
+ * Infinities and NaN become NaN, and leave their neighbours alone.
+ */
+int bbo_net_quantize(const void* x, int64_t x_stride, const void* gate, int64_t gate_stride, int64_t rows, int64_t cols,
+                     int32_t dtype, int32_t tile, void* q, int64_t q_stride, void* scales, int64_t scale_stride, void* qt,
+                     int64_t qt_stride, void* t_scales, int64_t t_scale_stride, void* stream);
+
+/* Bytes of workspace for bbo_net_matmul8 (0 for most shapes); writes *out. */
+int bbo_net_matmul8_workspace(int64_t m, int64_t n, int64_t k, size_t* out);
+
+/*
+ * c = a b^T, or c += a b^T: both operands have the contracted index along their rows, as bbo_net_quantize gives them
+ * (y = x w^T from x and w; the data gradient from dy and w's transpose; the weight gradient from the transposes of dy
+ * and x).
+ *   a, b     8-bit matrices [m][k] and [n][k] with tiles 1 or 128
+ *   c        [m][n], float32 or bfloat16 (c_dtype); accumulate != 0 adds to what is there
+ * Sums are in float32 and rounded once.  float32 output has float32's accuracy; for bfloat16 output the matrix
+ * units drop what a product has below 2^-13 of the largest among eight neighbours of the contracted index (about 1.4e-5 of
+ * the result on normal data, which the output's own rounding hides).  k = 0 gives zeros (or leaves c as it is).
+ *   workspace  16-byte aligned, bbo_net_matmul8_workspace() bytes; with less the same product takes longer
+ */
+int bbo_net_matmul8(const void* a, int64_t a_stride, const void* a_scales, int64_t a_scale_stride, int32_t a_tile, const void* b,
+                    int64_t b_stride, const void* b_scales, int64_t b_scale_stride, int32_t b_tile, int64_t m, int64_t n,
+                    int64_t k, void* c, int64_t c_stride, int32_t c_dtype, int32_t accumulate, void* workspace,
+                    size_t workspace_bytes, void* stream);
+
+/* One tensor of a model.  POD; the array is host memory, read during the call. */
+typedef struct bbo_net_tensor {
+  void* p;        /* parameters, p_dtype [n] */
+  const void* g;  /* gradient, g_dtype [n] */
+  void* m;        /* first moment: float32 [n], or e4m3 [n] */
+  void* v;        /* second moment: float32 [n], or e4m3 [n] */
+  float* m_scales; /* 8 bits: float32 [ceil(n / 128)], zeros with zero codes at the start */
+  float* v_scales;
+  void* copy;     /* bfloat16 [n] copy of the updated float32 parameters, or NULL */
+  int64_t n;
+  float lr, weight_decay;
+} bbo_net_tensor;
+
+/*
+ * One AdamW step over all tensors of a model, in place:
+ *   g' = g * grad_scale;  m = beta1 m + (1 - beta1) g';  v = beta2 v + (1 - beta2) g'^2
+ *   p = p - lr weight_decay p - lr (m / (1 - beta1^step)) / (sqrt(v / (1 - beta2^step)) + eps)
+ *   p_dtype, g_dtype   BBO_F32 | BBO_BF16 (bfloat16 parameters are rounded to nearest: a step below half of a
+ *                      parameter's last bit is lost; float32 parameters with a bfloat16 copy keep it)
+ *   moments            BBO_NET_MOMENTS_*
+ *   step               1, 2, ...
+ *   grad_scale         float32 [1], or NULL for 1
+ * 8-bit moments: both are updated in float32, used, and then held as e4m3 codes times a float32 scale per 128 values, rounded
+ * up or down at random with the probability of the distance, so that small changes are kept on the average.  The second
+ * moment's scale decays by beta2 itself and otherwise moves by powers of two only: what decays keeps its code, and only what
+ * a gradient adds is rounded.  A second moment that is not zero keeps a code that is not zero.  The random numbers are a
+ * function of seed, step, the tensor's index and the value's index.
+ * The call is a launch for each 40 tensors.
+ */
+int bbo_net_adamw(const bbo_net_tensor* tensors, int32_t count, int32_t p_dtype, int32_t g_dtype, int32_t moments, double beta1,
+                  double beta2, double eps, int64_t step, uint64_t seed, const float* grad_scale, void* stream);
+
+/* Message of the calling thread's last failed bbo_net_ call ("" if none). */
+const char* bbo_net_last_error(void);
+
+#ifdef __cplusplus
+}
+#endif
+#endif /* BBO_NET_H */

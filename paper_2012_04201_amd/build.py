@@ -9,7 +9,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libbbo_mlp.so")
 SOURCES = ["kernels_tiled.hip", "kernels_deep3.hip", "kernels_deep2.hip", "kernels_mid.hip", "kernels_full.hip", "kernels_small2.hip",
-           "kernels_small1.hip", "kernels_small3.hip", "kernels_small4.hip", "kernels_linear_lds.hip", "kernels_linear.hip", "bbo_mlp.hip"]
+           "kernels_small1.hip", "kernels_small3.hip", "kernels_small4.hip", "kernels_linear_lds.hip", "kernels_linear.hip", "bbo_mlp.hip",
+           "net_matmul8.hip", "net_norm.hip", "net_quant.hip", "net_adamw.hip", "net_error.hip"]
 FLAGS = ["-O3", "--offload-arch=gfx950", "-std=c++17", "-fPIC",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops", "-Wall", "-Wno-unused-function"]
 

@@ -1,0 +1,209 @@
+// AdamW over all tensors of a model in few launches, with moments in float32 or in 8 bits.
+#include "net_common.h"
+
+// The scales of 8-bit moments are bit-exact functions of the inputs: every product and sum is rounded by itself.
+#pragma clang fp contract(off)
+
+namespace {
+
+constexpr int TABLE = 40;  // tensors per launch: their records are kernel arguments (at most 4 KB)
+constexpr int CHUNK = 2048;  // values per workgroup: 256 threads with eight each
+
+struct AdamTensor {
+  void* p;
+  const void* g;
+  void *m, *v;
+  float *ms, *vs;
+  bf16* copy;
+  int64_t n;
+  uint64_t key;
+  float keep, step;  // 1 - lr weight_decay; lr / (1 - beta1^step)
+};
+struct AdamArgs {
+  AdamTensor t[TABLE];
+  int64_t first[TABLE + 1];  // chunks before tensor i
+  const float* grad_scale;
+  float b1, b2, c1, c2, eps, rbc2;  // c = 1 - b; rbc2 = 1 / sqrt(1 - beta2^step)
+  int count;
+};
+static_assert(sizeof(AdamArgs) <= 4096, "kernel arguments");
+
+__host__ __device__ inline uint64_t mix64(uint64_t z) {  // SplitMix64's output function
+  z = (z ^ (z >> 30)) * 0xBF58476D1CE4E5B9ull;
+  z = (z ^ (z >> 27)) * 0x94D049BB133111EBull;
+  return z ^ (z >> 31);
+}
+constexpr uint64_t GOLDEN = 0x9E3779B97F4A7C15ull;
+inline uint64_t key_fold(uint64_t h, uint64_t v) { return mix64(h + (v + 1) * GOLDEN); }
+
+// e4m3 code of |t| <= 448: the lower or the upper of the two values around it, the upper with the probability of t's distance
+// from the lower (to 16 bits).  2^-120 moves e4m3's exponent range to the low end of float32's, subnormals included, where
+// the code is the upper bits.
+__device__ inline uint32_t round_random(float t, uint32_t r16, uint32_t least) {
+  const float a = __builtin_fabsf(t);
+  uint32_t code = (as_u32(a * 0x1p-120f) + (r16 << 4)) >> 20;
+  code = a > 0.f && code < least ? least : code;
+  code = a < __builtin_inff() ? code : 127;
+  return code | (t < 0.f ? 128u : 0u);
+}
+__device__ inline float from_code(uint32_t byte) {
+  const float a = as_f32((byte & 127) << 20) * 0x1p120f;
+  return (byte & 127) == 127 ? __builtin_nanf("") : byte & 128 ? -a : a;
+}
+__device__ inline void load_codes(const uint8_t* p, int here, uint32_t (&w)[2]) {
+  if (here >= 8) {
+    const u32x2_any a = *(const u32x2_any*)p;
+    w[0] = a[0];
+    w[1] = a[1];
+  } else {
+    w[0] = w[1] = 0;
+#pragma unroll
+    for (int i = 0; i < 8; i++)
+      if (i < here) w[i >> 2] |= (uint32_t)p[i] << (8 * (i & 3));
+  }
+}
+
+template <typename P, typename G, bool EIGHT>
+__global__ __launch_bounds__(256) void k_adamw(const AdamArgs a) {
+  int lo = 0, hi = a.count;  // the tensor of this chunk: the last whose first chunk is not past it
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if ((int64_t)blockIdx.x < a.first[mid]) hi = mid;
+    else lo = mid;
+  }
+  const AdamTensor& t = a.t[lo];
+  const int64_t i0 = ((int64_t)blockIdx.x - a.first[lo]) * CHUNK + threadIdx.x * 8;
+  const int64_t left = t.n - i0;
+  const int here = left > 8 ? 8 : left < 0 ? 0 : (int)left;
+  const float gs = a.grad_scale ? *a.grad_scale : 1.f;
+  float p[8], g[8], m[8], v[8];
+  load8((const P*)t.p + i0, here, p);
+  load8((const G*)t.g + i0, here, g);
+#pragma unroll
+  for (int i = 0; i < 8; i++) g[i] *= gs;
+  if constexpr (EIGHT) {
+    // 16 lanes hold a block of 128
+    const int64_t b = i0 >> 7;
+    const float ms = here > 0 ? t.ms[b] : 0.f, vs = here > 0 ? t.vs[b] : 0.f;
+    uint32_t wm[2], wv[2];
+    load_codes((const uint8_t*)t.m + i0, here, wm);
+    load_codes((const uint8_t*)t.v + i0, here, wv);
+    const float old = fmaxf(vs * a.b2, 0x1p-100f);
+    float mtop = 0.f, vtop = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; i++) {
+      m[i] = from_code(wm[i >> 2] >> (8 * (i & 3)) & 255) * ms * a.b1 + g[i] * a.c1;
+      v[i] = from_code(wv[i >> 2] >> (8 * (i & 3)) & 255) * old + g[i] * g[i] * a.c2;
+      mtop = fmaxf(mtop, finite_abs(m[i]));
+      vtop = fmaxf(vtop, finite_abs(v[i]));
+    }
+    mtop = max16(mtop);
+    vtop = max16(vtop);
+    // The first moment's scale: the power of two that brings the largest into (224, 448].
+    int me = scale_byte(mtop);
+    me = me < 27 ? 27 : me;  // (2^-100)
+    const float ms_new = as_f32((uint32_t)me << 23);
+    // The second moment's: the decayed scale's mantissa with such an exponent.
+    const uint32_t tb = as_u32(vtop), ob = as_u32(old) & 0x7fffff;
+    const float tm = as_f32((tb & 0x7fffff) | 0x3f800000), om = as_f32(ob | 0x3f800000);
+    int ve = (int)(tb >> 23) - 7 - (tm <= 1.75f * om) - (tm <= 0.875f * om);
+    ve = ve < 27 ? 27 : ve;
+    const float vs_new = as_f32((uint32_t)ve << 23 | ob);
+    const float mi = 1.f / ms_new, vi = 1.f / vs_new;
+    uint32_t cm[2] = {}, cv[2] = {};
+#pragma unroll
+    for (int i = 0; i < 8; i += 2) {
+      const uint64_t r = mix64(t.key + (uint64_t)((i0 + i) / 2 + 1) * GOLDEN);
+#pragma unroll
+      for (int k = 0; k < 2; k++) {
+        const uint32_t rr = (uint32_t)(r >> (32 * k));
+        cm[(i + k) >> 2] |= round_random(m[i + k] * mi, rr & 0xffff, 0) << (8 * ((i + k) & 3));
+        cv[(i + k) >> 2] |= round_random(v[i + k] * vi, rr >> 16, 1) << (8 * ((i + k) & 3));
+      }
+    }
+    store8_bytes((uint8_t*)t.m + i0, here, cm[0], cm[1]);
+    store8_bytes((uint8_t*)t.v + i0, here, cv[0], cv[1]);
+    if ((threadIdx.x & 15) == 0 && here > 0) {
+      t.ms[b] = ms_new;
+      t.vs[b] = vs_new;
+    }
+  } else {
+    load8((const float*)t.m + i0, here, m);
+    load8((const float*)t.v + i0, here, v);
+#pragma unroll
+    for (int i = 0; i < 8; i++) {
+      m[i] = m[i] * a.b1 + g[i] * a.c1;
+      v[i] = v[i] * a.b2 + g[i] * g[i] * a.c2;
+    }
+    store8((float*)t.m + i0, here, m);
+    store8((float*)t.v + i0, here, v);
+  }
+#pragma unroll
+  for (int i = 0; i < 8; i++) p[i] = p[i] * t.keep - t.step * (m[i] / (sqrtf(v[i]) * a.rbc2 + a.eps));
+  store8((P*)t.p + i0, here, p);
+  if (t.copy) store8(t.copy + i0, here, p);
+}
+
+template <typename P, typename G>
+void launch(const AdamArgs& a, bool eight, hipStream_t s) {
+  const dim3 grid((uint32_t)a.first[a.count]);
+  if (eight) hipLaunchKernelGGL((k_adamw<P, G, true>), grid, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((k_adamw<P, G, false>), grid, dim3(256), 0, s, a);
+}
+
+}  // namespace
+
+extern "C" int bbo_net_adamw(const bbo_net_tensor* tensors, int32_t count, int32_t p_dtype, int32_t g_dtype, int32_t moments,
+                             double beta1, double beta2, double eps, int64_t step, uint64_t seed, const float* grad_scale,
+                             void* stream) {
+  net_begin();
+  if (count < 0) return net_fail(BBO_INVALID_ARG, "count < 0");
+  if (!float_type(p_dtype) || !float_type(g_dtype)) return net_fail(BBO_INVALID_ARG, "unknown dtype");
+  if (moments != BBO_NET_MOMENTS_F32 && moments != BBO_NET_MOMENTS_8BIT) return net_fail(BBO_INVALID_ARG, "unknown moments");
+  if (!(beta1 >= 0.0 && beta1 < 1.0 && beta2 >= 0.0 && beta2 < 1.0)) return net_fail(BBO_INVALID_ARG, "a beta is outside [0, 1)");
+  if (!(eps >= 0.0)) return net_fail(BBO_INVALID_ARG, "eps must be at least 0");
+  if (step < 1) return net_fail(BBO_INVALID_ARG, "step < 1");
+  if (count > 0 && !tensors) return net_fail(BBO_INVALID_ARG, "tensors is null");
+  const bool eight = moments == BBO_NET_MOMENTS_8BIT;
+  for (int32_t i = 0; i < count; i++) {
+    const bbo_net_tensor& t = tensors[i];
+    if (t.n < 0) return net_fail(BBO_INVALID_ARG, "n < 0");
+    if (t.n > (1ll << 40)) return net_fail(BBO_UNSUPPORTED, "tensor too large");
+    if (!(t.lr == t.lr && t.weight_decay == t.weight_decay)) return net_fail(BBO_INVALID_ARG, "lr or weight_decay is NaN");
+    if (t.n > 0 && (!t.p || !t.g || !t.m || !t.v)) return net_fail(BBO_INVALID_ARG, "p/g/m/v is null");
+    if (t.n > 0 && eight && (!t.m_scales || !t.v_scales)) return net_fail(BBO_INVALID_ARG, "8-bit moments have scales");
+    if (t.copy && p_dtype != BBO_F32) return net_fail(BBO_INVALID_ARG, "a copy is of float32 parameters");
+  }
+  const uint64_t key = key_fold(seed, (uint64_t)step);
+  const double bc1 = 1.0 - __builtin_pow(beta1, (double)step), bc2 = 1.0 - __builtin_pow(beta2, (double)step);
+  AdamArgs a;
+  a.grad_scale = grad_scale;
+  a.b1 = (float)beta1;
+  a.b2 = (float)beta2;
+  a.c1 = (float)(1.0 - beta1);
+  a.c2 = (float)(1.0 - beta2);
+  a.eps = (float)eps;
+  a.rbc2 = (float)(1.0 / __builtin_sqrt(bc2));
+  a.count = 0;
+  a.first[0] = 0;
+  for (int32_t i = 0; i < count; i++) {
+    const bbo_net_tensor& t = tensors[i];
+    if (t.n > 0) {
+      a.t[a.count] = AdamTensor{t.p, t.g, t.m, t.v, t.m_scales, t.v_scales, (bf16*)t.copy, t.n, key_fold(key, (uint64_t)i),
+                                (float)(1.0 - (double)t.lr * (double)t.weight_decay), (float)((double)t.lr / bc1)};
+      a.first[a.count + 1] = a.first[a.count] + ceil_div(t.n, CHUNK);
+      a.count++;
+    }
+    // (a grid has 31 bits of workgroups; 2^40 values are 2^29 chunks)
+    if (a.count > 0 && (a.count == TABLE || a.first[a.count] > (1 << 29) || i + 1 == count)) {
+      hipStream_t s = (hipStream_t)stream;
+      if (p_dtype == BBO_F32 && g_dtype == BBO_F32) launch<float, float>(a, eight, s);
+      else if (p_dtype == BBO_F32) launch<float, bf16>(a, eight, s);
+      else if (g_dtype == BBO_F32) launch<bf16, float>(a, eight, s);
+      else launch<bf16, bf16>(a, eight, s);
+      if (int rc = net_launched()) return rc;
+      a.count = 0;
+    }
+  }
+  return BBO_OK;
+}

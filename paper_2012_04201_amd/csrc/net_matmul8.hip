@@ -1,0 +1,369 @@
+// Product of two matrices in 8 bits with a power of two for each block of 128 of the contracted index: c = a b^T.
+//
+// bfloat16 output: the 8-bit matrix instruction, 16 x 16 x 128 with a scale for each operand row, so that a block's scale
+// goes in with its products and the sum stays in one set of float32 accumulators.  Within eight neighbours of the
+// contracted index the instruction keeps products to 2^-13 of the largest and drops what is below (measured: a product
+// of 15/16 2^-12 of another adds 8/15 of itself beside it, nothing further away than eight; sums of eights are
+// float32).  On normal data that is 1.4e-5 of the result, a hundredth of bfloat16's rounding.
+// float32 output: the same products on the bfloat16 instruction, whose operands hold an e4m3 value times its scale exactly
+// and whose products and sums are float32: half the rate, 1e-7.
+//
+// The instructions' first operand is b and the second a: a lane then holds four neighbouring columns of one row of c.
+#include "net_common.h"
+
+namespace {
+
+struct MatArgs {
+  const uint8_t *a, *as, *b, *bs;
+  void* c;
+  int64_t a_stride, as_stride, b_stride, bs_stride, c_stride;
+  int64_t m, n, k;
+  int a_shift, b_shift;  // a scale's row is the row >> shift
+  int c_f32, accumulate, direct;
+};
+
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+
+__device__ inline f32x4 mfma8(i32x8 b, i32x8 a, f32x4 c, int sb, int sa) {
+  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b, a, c, 0, 0, 0, sb, 0, sa);
+}
+
+// 32 codes of a row as bfloat16, times a power of two.
+struct Wide {
+  bf16x8 v[4];
+};
+__device__ inline Wide widen(i32x8 x, float scale) {
+  Wide w;
+#pragma unroll
+  for (int i = 0; i < 4; i++) {
+    const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x[2 * i], scale, false);
+    const bf16x2 b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x[2 * i], scale, true);
+    const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x[2 * i + 1], scale, false);
+    const bf16x2 d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x[2 * i + 1], scale, true);
+    w.v[i] = bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+  }
+  return w;
+}
+__device__ inline f32x4 mfma16(const Wide& b, const Wide& a, f32x4 c) {
+#pragma unroll
+  for (int i = 0; i < 4; i++) c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b.v[i], a.v[i], c, 0, 0, 0);
+  return c;
+}
+__device__ inline float scale_of(int byte) {  // 2^(byte - 127), NaN for 255
+  const uint32_t b = (uint32_t)byte;
+  return as_f32(b == 255 ? 0x7fc00000u : b == 0 ? 0x00400000u : b << 23);
+}
+// Scales that go into bfloat16 operands: with others an operand would leave that type's range, and the block's products are scaled after
+// their sum.
+__device__ inline bool in_range(int byte) { return (uint32_t)(byte - 27) <= 200u; }
+
+// 16 bytes of a row from byte `at`, zeros past the row's end.
+__device__ inline i32x4 load16(const uint8_t* row, int64_t at, int64_t k) {
+  if (at + 16 <= k) return __builtin_bit_cast(i32x4, *(const u32x4_any*)(row + at));
+  i32x4 v = {0, 0, 0, 0};
+  for (int i = 0; at + i < k && i < 16; i++) v[i >> 2] |= (int)row[at + i] << (8 * (i & 3));
+  return v;
+}
+
+// Four neighbouring values of c from column n on.
+__device__ inline void put4(const MatArgs& g, int64_t m, int64_t n, f32x4 v) {
+  if (m >= g.m || n >= g.n) return;
+  const int here = g.n - n >= 4 ? 4 : (int)(g.n - n);
+  if (g.c_f32) {
+    float* c = (float*)g.c + m * g.c_stride + n;
+    if (here == 4) {
+      if (g.accumulate) {
+        const u32x4_any o = *(const u32x4_any*)c;
+#pragma unroll
+        for (int i = 0; i < 4; i++) v[i] += as_f32(o[i]);
+      }
+      *(u32x4_any*)c = __builtin_bit_cast(u32x4_any, v);
+    } else {
+      for (int i = 0; i < here; i++) c[i] = g.accumulate ? c[i] + v[i] : v[i];
+    }
+  } else {
+    bf16* c = (bf16*)g.c + m * g.c_stride + n;
+    if (here == 4) {
+      if (g.accumulate) {
+        const u32x2_any o = *(const u32x2_any*)c;
+#pragma unroll
+        for (int i = 0; i < 4; i++) v[i] += to_f32((bf16)(o[i >> 1] >> (16 * (i & 1))));
+      }
+      u32x2_any w;
+      w[0] = (uint32_t)from_f32<bf16>(v[0]) | (uint32_t)from_f32<bf16>(v[1]) << 16;
+      w[1] = (uint32_t)from_f32<bf16>(v[2]) | (uint32_t)from_f32<bf16>(v[3]) << 16;
+      *(u32x2_any*)c = w;
+    } else {
+      for (int i = 0; i < here; i++) c[i] = from_f32<bf16>(g.accumulate ? to_f32(c[i]) + v[i] : v[i]);
+    }
+  }
+}
+
+// Products of one block of 128 for MI x NI tiles of 16 x 16, added to acc.  get_a(i), get_b(j): a lane's 32 codes of a row;
+// sa, sb: the rows' scales.
+template <bool EXACT, int MI, int NI, typename A, typename B>
+__device__ inline void block_products(f32x4 (&acc)[MI][NI], const int (&sa)[MI], const int (&sb)[NI], A get_a, B get_b) {
+  if constexpr (!EXACT) {
+    i32x8 b[NI];
+#pragma unroll
+    for (int j = 0; j < NI; j++) b[j] = get_b(j);
+#pragma unroll
+    for (int i = 0; i < MI; i++) {
+      const i32x8 a = get_a(i);
+#pragma unroll
+      for (int j = 0; j < NI; j++) acc[i][j] = mfma8(b[j], a, acc[i][j], sb[j], sa[i]);
+    }
+  } else {
+    bool ok = true;
+#pragma unroll
+    for (int i = 0; i < MI; i++) ok &= in_range(sa[i]);
+#pragma unroll
+    for (int j = 0; j < NI; j++) ok &= in_range(sb[j]);
+    const bool all = __all(ok);
+    Wide b[NI];
+#pragma unroll
+    for (int j = 0; j < NI; j++) b[j] = widen(get_b(j), all ? scale_of(sb[j]) : 1.f);
+    if (all) {
+#pragma unroll
+      for (int i = 0; i < MI; i++) {
+        const Wide a = widen(get_a(i), scale_of(sa[i]));
+#pragma unroll
+        for (int j = 0; j < NI; j++) acc[i][j] = mfma16(b[j], a, acc[i][j]);
+      }
+    } else {
+      const int q4 = (threadIdx.x & 63) >> 4 << 2;
+#pragma unroll
+      for (int i = 0; i < MI; i++) {
+        const Wide a = widen(get_a(i), 1.f);
+        const float s = scale_of(sa[i]);
+#pragma unroll
+        for (int j = 0; j < NI; j++) {
+          const f32x4 t = mfma16(b[j], a, f32x4{0.f, 0.f, 0.f, 0.f});
+#pragma unroll
+          for (int r = 0; r < 4; r++) acc[i][j][r] += t[r] * (s * scale_of(__shfl(sb[j], q4 + r)));
+        }
+      }
+    }
+  }
+}
+
+// Four scales of a row from block kb on, those past the row's end as 127; block kb + i in bits 8 i.
+__device__ inline uint32_t load_scales(const uint8_t* row, int64_t kb, int64_t blocks) {
+  typedef uint32_t u32_any __attribute__((aligned(1)));
+  if (kb + 4 <= blocks) return *(const u32_any*)(row + kb);
+  uint32_t v = 0x7f7f7f7f;
+  for (int i = 0; kb + i < blocks; i++) v = (v & ~(255u << (8 * i))) | (uint32_t)row[kb + i] << (8 * i);
+  return v;
+}
+
+// ---------------------------------------------------------------------------
+// Few rows: 16 columns of c a workgroup, whose waves share the contracted index.  Bound by the bytes of b, which go straight
+// to registers.
+// ---------------------------------------------------------------------------
+template <bool EXACT, int MT, int W>
+__global__ __launch_bounds__(64 * W) void k_mm_rows(const MatArgs g) {
+  __shared__ f32x4 part[W][MT][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r16 = lane & 15, q = lane >> 4;
+  const int64_t n0 = (int64_t)blockIdx.x * 16;
+  const int64_t nr = n0 + r16 < g.n ? n0 + r16 : g.n - 1;
+  const uint8_t* b = g.b + nr * g.b_stride;
+  const uint8_t* bs = g.bs + (nr >> g.b_shift) * g.bs_stride;
+  const uint8_t *a[MT], *as[MT];
+#pragma unroll
+  for (int t = 0; t < MT; t++) {
+    const int64_t mr = t * 16 + r16 < g.m ? t * 16 + r16 : g.m - 1;
+    a[t] = g.a + mr * g.a_stride;
+    as[t] = g.as + (mr >> g.a_shift) * g.as_stride;
+  }
+  f32x4 acc[MT][1] = {};
+  const int64_t blocks = ceil_div_d(g.k, 128);
+  auto codes = [&](const uint8_t* row, int64_t at) {
+    const i32x4 lo = load16(row, at, g.k), hi = load16(row, at + 16, g.k);
+    return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+  };
+  for (int64_t kb = wave; kb < blocks; kb += W) {
+    const int64_t at = kb * 128 + q * 32;
+    int sa[MT];
+    const int sb[1] = {bs[kb]};
+#pragma unroll
+    for (int t = 0; t < MT; t++) sa[t] = as[t][kb];
+    block_products<EXACT, MT, 1>(acc, sa, sb, [&](int t) { return codes(a[t], at); }, [&](int) { return codes(b, at); });
+  }
+#pragma unroll
+  for (int t = 0; t < MT; t++) part[wave][t][lane] = acc[t][0];
+  __syncthreads();
+  if (wave < MT) {
+    f32x4 s = part[0][wave][lane];
+#pragma unroll
+    for (int w = 1; w < W; w++) s += part[w][wave][lane];
+    put4(g, wave * 16 + r16, n0 + q * 4, s);
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Tiles of BM x BN, WM x WN waves.  Both operands' 128-byte rows go through LDS, two blocks of the contracted index in turn.
+// A row's eight 16-byte pieces are stored at piece ^ f(row), f = (row & 7) ^ (row >> 3 & 1): the 16 rows that a read takes
+// side by side then fall on different banks.  Whole blocks of rows at multiples of 16 bytes go from global memory to LDS by
+// themselves (g.direct); a last part of a block, and rows at other addresses, through registers.
+// ---------------------------------------------------------------------------
+__device__ inline int mix(int row) { return (row & 7) ^ (row >> 3 & 1); }
+
+template <bool EXACT, int BM, int BN, int WM, int WN>
+__global__ __launch_bounds__(64 * WM * WN) void k_mm_tile(const MatArgs g, int tiles_m, int tiles_n) {
+  constexpr int W = WM * WN, MI = BM / WM / 16, NI = BN / WN / 16;
+  __shared__ __attribute__((aligned(128))) uint8_t lds[2][(BM + BN) * 128];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r16 = lane & 15, q = lane >> 4;
+  const int wm = wave / WN, wn = wave % WN;
+  const int tile_m = blockIdx.x % tiles_m, tile_n = blockIdx.x / tiles_m;
+  const int64_t m0 = (int64_t)tile_m * BM, n0 = (int64_t)tile_n * BN;
+  const int64_t blocks = ceil_div_d(g.k, 128), direct = g.direct ? g.k >> 7 : 0;
+
+  // Rows of the two operands, one after the other: [0, BM) of a, [BM, BM + BN) of b; those past the end repeat the last.
+  auto row_of = [&](int r) -> const uint8_t* {
+    if (r < BM) {
+      const int64_t m = m0 + r < g.m ? m0 + r : g.m - 1;
+      return g.a + m * g.a_stride;
+    }
+    const int64_t n = n0 + r - BM < g.n ? n0 + r - BM : g.n - 1;
+    return g.b + n * g.b_stride;
+  };
+  constexpr int LOADS = (BM + BN) / 8 / W;  // of 8 rows each by a wave
+  const uint8_t* from[LOADS];
+#pragma unroll
+  for (int j = 0; j < LOADS; j++) {
+    const int r = (j * W + wave) * 8 + (lane >> 3);
+    from[j] = row_of(r) + ((lane & 7) ^ mix(r)) * 16;
+  }
+  auto stage = [&](int64_t kb, int to) {
+#pragma unroll
+    for (int j = 0; j < LOADS; j++)
+      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(from[j] + kb * 128),
+                                       (__attribute__((address_space(3))) void*)&lds[to][(j * W + wave) * 1024], 16, 0, 0);
+  };
+  const uint8_t *as[MI], *bs[NI];
+  uint32_t sa4[MI], sb4[NI], sa_next[MI], sb_next[NI];
+#pragma unroll
+  for (int i = 0; i < MI; i++) {
+    const int64_t m = m0 + wm * (BM / WM) + i * 16 + r16;
+    as[i] = g.as + ((m < g.m ? m : g.m - 1) >> g.a_shift) * g.as_stride;
+    sa_next[i] = sa4[i] = load_scales(as[i], 0, blocks);
+  }
+#pragma unroll
+  for (int i = 0; i < NI; i++) {
+    const int64_t n = n0 + wn * (BN / WN) + i * 16 + r16;
+    bs[i] = g.bs + ((n < g.n ? n : g.n - 1) >> g.b_shift) * g.bs_stride;
+    sb_next[i] = sb4[i] = load_scales(bs[i], 0, blocks);
+  }
+  f32x4 acc[MI][NI] = {};
+  const int p0 = (q * 2 ^ mix(r16)) * 16, p1 = ((q * 2 + 1) ^ mix(r16)) * 16;
+  auto products = [&](int64_t kb, int in) {
+    auto frag = [&](int row16) {
+      const uint8_t* at = &lds[in][(row16 + r16) * 128];
+      const i32x4 lo = *(const i32x4*)(at + p0), hi = *(const i32x4*)(at + p1);
+      return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+    };
+    const int shift = (int)(kb & 3) * 8;
+    int sa[MI], sb[NI];
+#pragma unroll
+    for (int i = 0; i < MI; i++) sa[i] = sa4[i] >> shift & 255;
+#pragma unroll
+    for (int i = 0; i < NI; i++) sb[i] = sb4[i] >> shift & 255;
+    block_products<EXACT, MI, NI>(acc, sa, sb, [&](int i) { return frag(wm * (BM / WM) + i * 16); },
+                                  [&](int j) { return frag(BM + wn * (BN / WN) + j * 16); });
+  };
+  // The scales of the four blocks from kb on; asked for four blocks ahead.
+  auto next_scales = [&](int64_t kb) {
+    if ((kb & 3) == 0) {
+#pragma unroll
+      for (int i = 0; i < MI; i++) sa4[i] = sa_next[i], sa_next[i] = load_scales(as[i], kb + 4, blocks);
+#pragma unroll
+      for (int i = 0; i < NI; i++) sb4[i] = sb_next[i], sb_next[i] = load_scales(bs[i], kb + 4, blocks);
+    }
+  };
+  if (direct > 0) stage(0, 0);
+  for (int64_t kb = 0; kb < direct; kb++) {
+    __syncthreads();  // this block has landed, and the other half is free
+    next_scales(kb);
+    if (kb + 1 < direct) stage(kb + 1, (int)(kb + 1) & 1);
+    products(kb, (int)kb & 1);
+  }
+  for (int64_t kb = direct; kb < blocks; kb++) {
+    __syncthreads();
+    for (int j = 0; j < LOADS; j++) {
+      const int r = (j * W + wave) * 8 + (lane >> 3);
+      *(i32x4*)&lds[0][(j * W + wave) * 1024 + lane * 16] = load16(row_of(r), kb * 128 + ((lane & 7) ^ mix(r)) * 16, g.k);
+    }
+    next_scales(kb);
+    __syncthreads();
+    products(kb, 0);
+  }
+#pragma unroll
+  for (int i = 0; i < MI; i++)
+#pragma unroll
+    for (int j = 0; j < NI; j++)
+      put4(g, m0 + wm * (BM / WM) + i * 16 + r16, n0 + wn * (BN / WN) + j * 16 + q * 4, acc[i][j]);
+}
+
+template <bool EXACT, int MT>
+void rows(const MatArgs& g, hipStream_t s) {
+  hipLaunchKernelGGL((k_mm_rows<EXACT, MT, 8>), dim3((uint32_t)ceil_div(g.n, 16)), dim3(512), 0, s, g);
+}
+template <bool EXACT, int BM, int BN, int WM, int WN>
+void tiles(const MatArgs& g, hipStream_t s) {
+  const int tm = (int)ceil_div(g.m, BM), tn = (int)ceil_div(g.n, BN);
+  hipLaunchKernelGGL((k_mm_tile<EXACT, BM, BN, WM, WN>), dim3((uint32_t)((int64_t)tm * tn)), dim3(64 * WM * WN), 0, s, g, tm, tn);
+}
+template <bool EXACT>
+void launch(const MatArgs& g, hipStream_t s) {
+  if (g.m <= 16) rows<EXACT, 1>(g, s);
+  else if (g.m <= 32) rows<EXACT, 2>(g, s);
+  else if (g.m <= 64) rows<EXACT, 4>(g, s);
+  else if (ceil_div(g.m, 256) * ceil_div(g.n, 256) >= 192) tiles<EXACT, 256, 256, 2, 4>(g, s);
+  else if (ceil_div(g.m, 128) * ceil_div(g.n, 128) >= 192) tiles<EXACT, 128, 128, 2, 2>(g, s);
+  else tiles<EXACT, 64, 64, 2, 2>(g, s);
+}
+
+}  // namespace
+
+extern "C" {
+
+int bbo_net_matmul8_workspace(int64_t m, int64_t n, int64_t k, size_t* out) {
+  net_begin();
+  if (!out) return net_fail(BBO_INVALID_ARG, "out is null");
+  if (m < 0 || n < 0 || k < 0) return net_fail(BBO_INVALID_ARG, "m, n or k < 0");
+  *out = 0;
+  return BBO_OK;
+}
+
+int bbo_net_matmul8(const void* a, int64_t a_stride, const void* a_scales, int64_t a_scale_stride, int32_t a_tile, const void* b,
+                    int64_t b_stride, const void* b_scales, int64_t b_scale_stride, int32_t b_tile, int64_t m, int64_t n,
+                    int64_t k, void* c, int64_t c_stride, int32_t c_dtype, int32_t accumulate, void* workspace,
+                    size_t workspace_bytes, void* stream) {
+  net_begin();
+  if (m < 0 || n < 0 || k < 0) return net_fail(BBO_INVALID_ARG, "m, n or k < 0");
+  if ((a_tile != 1 && a_tile != 128) || (b_tile != 1 && b_tile != 128)) return net_fail(BBO_INVALID_ARG, "tile must be 1 or 128");
+  if (!float_type(c_dtype)) return net_fail(BBO_INVALID_ARG, "unknown dtype");
+  // (a grid's 31 bits of workgroups, the smallest 16 columns)
+  if (m > (1ll << 31) || n > (1ll << 31) || k > (1ll << 31) || ceil_div(m, 64) * ceil_div(n, 64) > 0x7fffffff)
+    return net_fail(BBO_UNSUPPORTED, "matrix too large");
+  if (m == 0 || n == 0) return BBO_OK;
+  if (!c) return net_fail(BBO_INVALID_ARG, "c is null");
+  if (c_stride < n) return net_fail(BBO_INVALID_ARG, "a stride is less than a row");
+  if (k > 0) {
+    if (!a || !b || !a_scales || !b_scales) return net_fail(BBO_INVALID_ARG, "a/b/scales is null");
+    if (a_stride < k || b_stride < k || a_scale_stride < ceil_div(k, 128) || b_scale_stride < ceil_div(k, 128))
+      return net_fail(BBO_INVALID_ARG, "a stride is less than a row");
+  }
+  (void)workspace;
+  (void)workspace_bytes;
+  const MatArgs g{(const uint8_t*)a, (const uint8_t*)a_scales, (const uint8_t*)b, (const uint8_t*)b_scales, c, a_stride,
+                  a_scale_stride, b_stride, b_scale_stride, c_stride, m, n, k, a_tile == 128 ? 7 : 0, b_tile == 128 ? 7 : 0,
+                  c_dtype == BBO_F32, accumulate != 0,
+                  !(((uintptr_t)a | (uintptr_t)b | (uint64_t)a_stride | (uint64_t)b_stride) & 15)};
+  if (g.c_f32) launch<true>(g, (hipStream_t)stream);
+  else launch<false>(g, (hipStream_t)stream);
+  return net_launched();
+}
+
+}  // extern "C"

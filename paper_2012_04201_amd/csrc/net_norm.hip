@@ -1,0 +1,294 @@
+// Root-mean-square norm of rows with the residual's addition and an output in 8 bits, and its gradient.
+#include "net_common.h"
+
+namespace {
+
+// A row is held by T threads in NV vectors of eight values each: vector v of thread t starts at column (v T + t) 8, so that
+// 16 lanes side by side hold a block of 128.  T = 64: a wave per row, four rows per workgroup.
+template <int T, int NV>
+struct RowCut {
+  static constexpr int PER_WG = T == 64 ? 4 : 1;
+  static constexpr int THREADS = T * PER_WG;
+  static __device__ int lane() { return threadIdx.x % T; }
+  static __device__ int64_t group() { return (int64_t)blockIdx.x * PER_WG + threadIdx.x / T; }
+  static __device__ int col(int v) { return (v * T + lane()) * 8; }
+};
+
+// Sum over a row's T threads, the same for all of them; `slots`: LDS of T / 64 floats, free again after a barrier.
+template <int T>
+__device__ inline float row_sum(float x, float* slots) {
+  x = wave_sum(x);
+  if constexpr (T > 64) {
+    const int w = threadIdx.x >> 6;
+    if ((threadIdx.x & 63) == 0) slots[w] = x;
+    __syncthreads();
+    x = 0.f;
+#pragma unroll
+    for (int i = 0; i < T / 64; i++) x += slots[i];
+  }
+  return x;
+}
+
+struct NormArgs {
+  const void *x, *residual;
+  const float* weight;
+  void *sum, *y;
+  float* rstd;
+  uint8_t *q, *q_scales;
+  int64_t x_stride, residual_stride, sum_stride, y_stride, q_stride, q_scale_stride, rows;
+  int width;
+  float eps;
+};
+
+// One pass: a row is read once, kept in registers over the reduction and written once.
+template <typename E, int T, int NV>
+__global__ __launch_bounds__(T == 64 ? 256 : T) void k_rms_norm(const NormArgs a) {
+  using C = RowCut<T, NV>;
+  __shared__ float slots[T > 64 ? T / 64 : 1];
+  const int64_t row = C::group();
+  if (T == 64 && row >= a.rows) return;  // (a wave of its own; with more threads per row there is a workgroup per row)
+  float h[NV][8];
+  const E* x = (const E*)a.x + row * a.x_stride;
+#pragma unroll
+  for (int v = 0; v < NV; v++) load8(x + C::col(v), a.width - C::col(v), h[v]);
+  if (a.residual) {
+    const E* r = (const E*)a.residual + row * a.residual_stride;
+    E* s = (E*)a.sum + row * a.sum_stride;
+#pragma unroll
+    for (int v = 0; v < NV; v++) {
+      float t[8];
+      load8(r + C::col(v), a.width - C::col(v), t);
+#pragma unroll
+      for (int i = 0; i < 8; i++) h[v][i] = to_f32(from_f32<E>(h[v][i] + t[i]));  // as it is kept
+      store8(s + C::col(v), a.width - C::col(v), h[v]);
+    }
+  }
+  float ss = 0.f;
+#pragma unroll
+  for (int v = 0; v < NV; v++)
+#pragma unroll
+    for (int i = 0; i < 8; i++) ss += h[v][i] * h[v][i];
+  const float rstd = rsqrtf(row_sum<T>(ss, slots) / (float)a.width + a.eps);
+  if (a.rstd && C::lane() == 0) a.rstd[row] = rstd;
+  if (!a.y && !a.q) return;
+#pragma unroll
+  for (int v = 0; v < NV; v++) {
+    const int c = C::col(v), here = a.width - c;
+    if (a.weight) {
+      float w[8];
+      load8(a.weight + c, here, w);
+#pragma unroll
+      for (int i = 0; i < 8; i++) h[v][i] = h[v][i] * rstd * w[i];
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; i++) h[v][i] *= rstd;
+    }
+    if (a.y) store8((E*)a.y + row * a.y_stride + c, here, h[v]);
+    if (a.q) {
+      float top = 0.f;
+#pragma unroll
+      for (int i = 0; i < 8; i++) top = fmaxf(top, finite_abs(h[v][i]));
+      const int byte = scale_byte(max16(top));
+      uint32_t lo, hi;
+      pack8_e4m3(h[v], inverse_scale(byte), lo, hi);
+      store8_bytes(a.q + row * a.q_stride + c, here, lo, hi);
+      if ((C::lane() & 15) == 0 && here > 0) a.q_scales[row * a.q_scale_stride + (c >> 7)] = (uint8_t)byte;
+    }
+  }
+}
+
+struct GradArgs {
+  const void *dy, *dsum, *h;
+  const float *rstd, *weight;
+  void* dx;
+  float* parts;  // [groups][width], or null
+  int64_t dy_stride, dsum_stride, h_stride, dx_stride, rows;
+  int width, groups;
+};
+
+// Each group of T threads takes every groups-th row and keeps its share of dweight in registers; k_dweight adds the groups'.
+template <typename E, int T, int NV>
+__global__ __launch_bounds__(T == 64 ? 256 : T) void k_rms_norm_grad(const GradArgs a) {
+  using C = RowCut<T, NV>;
+  __shared__ float slots[2][T > 64 ? T / 64 : 1];
+  const int64_t group = C::group();
+  if (T == 64 && group >= a.groups) return;
+  float dw[NV][8] = {};
+  int at = 0;
+  for (int64_t row = group; row < a.rows; row += a.groups, at ^= 1) {
+    const float rstd = a.rstd[row];
+    const E* pg = (const E*)a.dy + row * a.dy_stride;
+    const E* ph = (const E*)a.h + row * a.h_stride;
+    float g[NV][8], xh[NV][8];
+#pragma unroll
+    for (int v = 0; v < NV; v++) {
+      const int c = C::col(v), here = a.width - c;
+      load8(pg + c, here, g[v]);
+      load8(ph + c, here, xh[v]);
+    }
+    float dot = 0.f;
+#pragma unroll
+    for (int v = 0; v < NV; v++) {
+      float w[8];
+      if (a.weight) {
+        load8(a.weight + C::col(v), a.width - C::col(v), w);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 8; i++) w[i] = 1.f;
+      }
+#pragma unroll
+      for (int i = 0; i < 8; i++) {
+        xh[v][i] *= rstd;
+        dw[v][i] += g[v][i] * xh[v][i];
+        g[v][i] *= w[i];
+        dot += g[v][i] * xh[v][i];
+      }
+    }
+    // (two sets of slots: a wave may reach the next row's sum while another still reads this row's)
+    const float mean = row_sum<T>(dot, slots[at]) / (float)a.width;
+    const E* ps = a.dsum ? (const E*)a.dsum + row * a.dsum_stride : nullptr;
+    E* px = (E*)a.dx + row * a.dx_stride;
+#pragma unroll
+    for (int v = 0; v < NV; v++) {
+      const int c = C::col(v), here = a.width - c;
+      float d[8];
+      if (ps) {
+        load8(ps + c, here, d);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 8; i++) d[i] = 0.f;
+      }
+#pragma unroll
+      for (int i = 0; i < 8; i++) d[i] += rstd * (g[v][i] - xh[v][i] * mean);
+      store8(px + c, here, d);
+    }
+  }
+  if (a.parts) {
+#pragma unroll
+    for (int v = 0; v < NV; v++) store8(a.parts + group * a.width + C::col(v), a.width - C::col(v), dw[v]);
+  }
+}
+
+// dweight[c] = sum of the groups' shares, in a fixed order: 64 columns a workgroup, 16 waves that take every 16th group.
+__global__ __launch_bounds__(1024) void k_dweight(const float* parts, int groups, int width, float* dweight) {
+  __shared__ float part[16][64];
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, c = blockIdx.x * 64 + lane;
+  float s = 0.f;
+  if (c < width) {
+#pragma unroll 8
+    for (int g = w; g < groups; g += 16) s += parts[(int64_t)g * width + c];
+  }
+  part[w][lane] = s;
+  __syncthreads();
+  if (w == 0 && c < width) {
+    s = 0.f;
+#pragma unroll
+    for (int i = 0; i < 16; i++) s += part[i][lane];
+    dweight[c] = s;
+  }
+}
+
+// The cut by the width: as few threads as hold the row in registers.
+template <typename E, template <typename, int, int> class F, typename A>
+void by_width(int width, const A& a, hipStream_t s) {
+  if (width <= 512) F<E, 64, 1>::go(a, s);
+  else if (width <= 1024) F<E, 64, 2>::go(a, s);
+  else if (width <= 2048) F<E, 256, 1>::go(a, s);
+  else if (width <= 4096) F<E, 256, 2>::go(a, s);
+  else if (width <= 8192) F<E, 256, 4>::go(a, s);
+  else if (width <= 16384) F<E, 1024, 2>::go(a, s);
+  else F<E, 1024, 4>::go(a, s);
+}
+template <typename E, int T, int NV>
+struct Norm {
+  static void go(const NormArgs& a, hipStream_t s) {
+    using C = RowCut<T, NV>;
+    hipLaunchKernelGGL((k_rms_norm<E, T, NV>), dim3((uint32_t)ceil_div(a.rows, C::PER_WG)), dim3(C::THREADS), 0, s, a);
+  }
+};
+template <typename E, int T, int NV>
+struct Grad {
+  static void go(const GradArgs& a, hipStream_t s) {
+    using C = RowCut<T, NV>;
+    hipLaunchKernelGGL((k_rms_norm_grad<E, T, NV>), dim3((uint32_t)ceil_div(a.groups, C::PER_WG)), dim3(C::THREADS), 0, s, a);
+  }
+};
+
+// Groups of threads that share the rows of a gradient: 2048 waves' worth, at most one per row.
+int grad_groups(int64_t rows, int64_t width) {
+  const int most = width <= 1024 ? 2048 : width <= 8192 ? 1024 : 256;
+  return (int)(rows < most ? rows : most);
+}
+
+int check_rows(int64_t rows, int64_t width, int32_t dtype) {
+  if (rows < 0) return net_fail(BBO_INVALID_ARG, "rows < 0");
+  if (rows > 0x7fffffff) return net_fail(BBO_UNSUPPORTED, "rows too large");
+  if (width < 1) return net_fail(BBO_INVALID_ARG, "width < 1");
+  if (width > BBO_NET_MAX_WIDTH) return net_fail(BBO_UNSUPPORTED, "width > BBO_NET_MAX_WIDTH");
+  if (!float_type(dtype)) return net_fail(BBO_INVALID_ARG, "unknown dtype");
+  return BBO_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int bbo_net_rms_norm(const void* x, int64_t x_stride, const void* residual, int64_t residual_stride, const float* weight,
+                     int64_t rows, int64_t width, float eps, int32_t dtype, void* sum, int64_t sum_stride, void* y,
+                     int64_t y_stride, float* rstd, void* q, int64_t q_stride, void* q_scales, int64_t q_scale_stride,
+                     void* stream) {
+  net_begin();
+  if (int rc = check_rows(rows, width, dtype)) return rc;
+  if (!(eps >= 0.f)) return net_fail(BBO_INVALID_ARG, "eps must be at least 0");
+  if (!residual != !sum) return net_fail(BBO_INVALID_ARG, "residual and sum go together");
+  if (!q != !q_scales) return net_fail(BBO_INVALID_ARG, "q and q_scales go together");
+  if (rows == 0) return BBO_OK;
+  if (!x) return net_fail(BBO_INVALID_ARG, "x is null");
+  if (x_stride < width || (residual && (residual_stride < width || sum_stride < width)) || (y && y_stride < width) ||
+      (q && (q_stride < width || q_scale_stride < ceil_div(width, 128))))
+    return net_fail(BBO_INVALID_ARG, "a stride is less than a row");
+  const NormArgs a{x, residual, weight, sum, y, rstd, (uint8_t*)q, (uint8_t*)q_scales, x_stride, residual_stride, sum_stride,
+                   y_stride, q_stride, q_scale_stride, rows, (int)width, eps};
+  if (dtype == BBO_F32) by_width<float, Norm>((int)width, a, (hipStream_t)stream);
+  else by_width<bf16, Norm>((int)width, a, (hipStream_t)stream);
+  return net_launched();
+}
+
+int bbo_net_rms_norm_grad_workspace(int64_t rows, int64_t width, size_t* out) {
+  net_begin();
+  if (!out) return net_fail(BBO_INVALID_ARG, "out is null");
+  if (int rc = check_rows(rows, width, BBO_F32)) return rc;
+  *out = (size_t)grad_groups(rows, width) * (size_t)width * sizeof(float);
+  return BBO_OK;
+}
+
+int bbo_net_rms_norm_grad(const void* dy, int64_t dy_stride, const void* dsum, int64_t dsum_stride, const void* h,
+                          int64_t h_stride, const float* rstd, const float* weight, int64_t rows, int64_t width, int32_t dtype,
+                          void* dx, int64_t dx_stride, float* dweight, void* workspace, size_t workspace_bytes, void* stream) {
+  net_begin();
+  if (int rc = check_rows(rows, width, dtype)) return rc;
+  const int groups = grad_groups(rows, width);
+  hipStream_t s = (hipStream_t)stream;
+  if (rows > 0) {
+    if (!dy || !h || !rstd || !dx) return net_fail(BBO_INVALID_ARG, "dy/h/rstd/dx is null");
+    if (dy_stride < width || h_stride < width || dx_stride < width || (dsum && dsum_stride < width))
+      return net_fail(BBO_INVALID_ARG, "a stride is less than a row");
+    if (dweight && !workspace) return net_fail(BBO_INVALID_ARG, "workspace is null");
+    if (dweight && ((uintptr_t)workspace & 15)) return net_fail(BBO_INVALID_ARG, "workspace must be 16-byte aligned");
+    if (dweight && workspace_bytes < (size_t)groups * (size_t)width * sizeof(float))
+      return net_fail(BBO_WORKSPACE_TOO_SMALL, "workspace too small");
+    const GradArgs a{dy, dsum, h, rstd, weight, dx, dweight ? (float*)workspace : nullptr, dy_stride, dsum_stride, h_stride,
+                     dx_stride, rows, (int)width, groups};
+    if (dtype == BBO_F32) by_width<float, Grad>((int)width, a, s);
+    else by_width<bf16, Grad>((int)width, a, s);
+    if (int rc = net_launched()) return rc;
+  }
+  if (dweight) {
+    hipLaunchKernelGGL(k_dweight, dim3((uint32_t)ceil_div(width, 64)), dim3(1024), 0, s, (const float*)workspace, groups,
+                       (int)width, dweight);
+    return net_launched();
+  }
+  return BBO_OK;
+}
+
+}  // extern "C"

@@ -1,0 +1,171 @@
+// Matrices into 8 bits: e4m3 values with a power of two for each block of 128, in their own order, transposed, or both.
+#include "net_common.h"
+
+namespace {
+
+struct QuantArgs {
+  const void *x, *gate;
+  uint8_t *q, *s, *qt, *st;
+  int64_t x_stride, gate_stride, q_stride, s_stride, qt_stride, st_stride, rows, cols;
+};
+
+template <typename E>
+__device__ inline void load_gated(const QuantArgs& a, int64_t r, int64_t c, int here, float (&v)[8]) {
+  load8((const E*)a.x + r * a.x_stride + c, here, v);
+  if (a.gate) {
+    float g[8];
+    load8((const E*)a.gate + r * a.gate_stride + c, here, g);
+#pragma unroll
+    for (int i = 0; i < 8; i++) v[i] = g[i] <= 0.f ? 0.f : v[i];
+  }
+}
+__device__ inline int clip8(int64_t here) { return here > 8 ? 8 : here < 0 ? 0 : (int)here; }
+
+// Tile 1, own order only: 16 lanes hold a block, nothing is exchanged but its maximum.
+template <typename E>
+__global__ __launch_bounds__(256) void k_quant_rows(const QuantArgs a, int64_t blocks_per_row, int64_t blocks) {
+  const int64_t b = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4);
+  if (b >= blocks) return;
+  const int64_t r = b / blocks_per_row, kb = b - r * blocks_per_row, c = kb * 128 + (threadIdx.x & 15) * 8;
+  const int here = clip8(a.cols - c);
+  float v[8];
+  load_gated<E>(a, r, c, here, v);
+  float top = 0.f;
+#pragma unroll
+  for (int i = 0; i < 8; i++) top = fmaxf(top, finite_abs(v[i]));
+  const int byte = scale_byte(max16(top));
+  uint32_t lo, hi;
+  pack8_e4m3(v, inverse_scale(byte), lo, hi);
+  store8_bytes(a.q + r * a.q_stride + c, here, lo, hi);
+  if ((threadIdx.x & 15) == 0) a.s[r * a.s_stride + kb] = (uint8_t)byte;
+}
+
+// A workgroup takes 128 x 128 values; a thread keeps 8 x 8 of them in registers, so that either order's bytes come out of it
+// in groups of eight.  The transpose goes through LDS, so that global memory sees 128 bytes side by side.
+template <typename E, int TILE>
+__global__ __launch_bounds__(256) void k_quant_tile(const QuantArgs a) {
+  __shared__ float top_of[4][128];
+  __shared__ __attribute__((aligned(16))) uint32_t turned[128][32];  // [column][rows / 4]
+  const int l16 = threadIdx.x & 15, g = threadIdx.x >> 4, wave = threadIdx.x >> 6;
+  const int64_t r0 = (int64_t)blockIdx.y * 128, c0 = (int64_t)blockIdx.x * 128;
+  const int64_t c = c0 + l16 * 8;
+  const int here = clip8(a.cols - c);
+  float v[8][8];
+#pragma unroll
+  for (int i = 0; i < 8; i++) {
+    const int64_t r = r0 + g * 8 + i;
+    load_gated<E>(a, r < a.rows ? r : 0, c, r < a.rows ? here : 0, v[i]);
+  }
+  float col_top[8] = {}, row_top[8] = {};
+#pragma unroll
+  for (int i = 0; i < 8; i++)
+#pragma unroll
+    for (int j = 0; j < 8; j++) {
+      const float t = finite_abs(v[i][j]);
+      col_top[j] = fmaxf(col_top[j], t);
+      row_top[i] = fmaxf(row_top[i], t);
+    }
+  int byte128 = 0;
+  if (TILE == 128 || a.qt) {
+#pragma unroll
+    for (int j = 0; j < 8; j++) {  // over the wave's 32 rows
+      col_top[j] = fmaxf(col_top[j], __shfl_xor(col_top[j], 16));
+      col_top[j] = fmaxf(col_top[j], __shfl_xor(col_top[j], 32));
+    }
+    if ((threadIdx.x & 48) == 0) {
+#pragma unroll
+      for (int j = 0; j < 8; j++) top_of[wave][l16 * 8 + j] = col_top[j];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < 8; j++) {
+      const int k = l16 * 8 + j;
+      col_top[j] = fmaxf(fmaxf(top_of[0][k], top_of[1][k]), fmaxf(top_of[2][k], top_of[3][k]));
+    }
+    if (TILE == 128) {
+      float t = col_top[0];
+#pragma unroll
+      for (int j = 1; j < 8; j++) t = fmaxf(t, col_top[j]);
+      byte128 = scale_byte(max16(t));
+      if (threadIdx.x == 0) {
+        if (a.s) a.s[blockIdx.y * a.s_stride + blockIdx.x] = (uint8_t)byte128;
+        if (a.st) a.st[blockIdx.x * a.st_stride + blockIdx.y] = (uint8_t)byte128;
+      }
+    }
+  }
+  if (a.q) {
+#pragma unroll
+    for (int i = 0; i < 8; i++) {
+      const int64_t r = r0 + g * 8 + i;
+      const int byte = TILE == 128 ? byte128 : scale_byte(max16(row_top[i]));
+      uint32_t lo, hi;
+      pack8_e4m3(v[i], inverse_scale(byte), lo, hi);
+      if (r < a.rows) {
+        store8_bytes(a.q + r * a.q_stride + c, here, lo, hi);
+        if (TILE == 1 && l16 == 0) a.s[r * a.s_stride + blockIdx.x] = (uint8_t)byte;
+      }
+    }
+  }
+  if (a.qt) {
+#pragma unroll
+    for (int j = 0; j < 8; j++) {
+      const int k = l16 * 8 + j;
+      const int byte = TILE == 128 ? byte128 : scale_byte(col_top[j]);
+      float t[8];
+#pragma unroll
+      for (int i = 0; i < 8; i++) t[i] = v[i][j];
+      uint32_t lo, hi;
+      pack8_e4m3(t, inverse_scale(byte), lo, hi);
+      // groups of eight rows are swapped by the column's eight, so that 16 lanes' writes fall on different banks
+      uint32_t* to = &turned[k][(g ^ l16) * 2];
+      to[0] = lo;
+      to[1] = hi;
+      if (TILE == 1 && g == 0 && c0 + k < a.cols) a.st[(c0 + k) * a.st_stride + blockIdx.y] = (uint8_t)byte;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 8; i++) {
+      const int k = i * 16 + g;  // 16 lanes write a column's 128 rows
+      const uint32_t* from = &turned[k][(l16 ^ (k >> 3)) * 2];
+      const int64_t r = r0 + l16 * 8;
+      if (c0 + k < a.cols) store8_bytes(a.qt + (c0 + k) * a.qt_stride + r, clip8(a.rows - r), from[0], from[1]);
+    }
+  }
+}
+
+template <typename E>
+void launch(const QuantArgs& a, int tile, hipStream_t s) {
+  if (tile == 1 && !a.qt) {
+    const int64_t per_row = ceil_div(a.cols, 128), blocks = per_row * a.rows;
+    hipLaunchKernelGGL((k_quant_rows<E>), dim3((uint32_t)ceil_div(blocks, 16)), dim3(256), 0, s, a, per_row, blocks);
+    return;
+  }
+  const dim3 grid((uint32_t)ceil_div(a.cols, 128), (uint32_t)ceil_div(a.rows, 128));
+  if (tile == 1) hipLaunchKernelGGL((k_quant_tile<E, 1>), grid, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((k_quant_tile<E, 128>), grid, dim3(256), 0, s, a);
+}
+
+}  // namespace
+
+extern "C" int bbo_net_quantize(const void* x, int64_t x_stride, const void* gate, int64_t gate_stride, int64_t rows, int64_t cols,
+                                int32_t dtype, int32_t tile, void* q, int64_t q_stride, void* scales, int64_t scale_stride,
+                                void* qt, int64_t qt_stride, void* t_scales, int64_t t_scale_stride, void* stream) {
+  net_begin();
+  if (rows < 0 || cols < 0) return net_fail(BBO_INVALID_ARG, "rows < 0 or cols < 0");
+  if (!float_type(dtype)) return net_fail(BBO_INVALID_ARG, "unknown dtype");
+  if (tile != 1 && tile != 128) return net_fail(BBO_INVALID_ARG, "tile must be 1 or 128");
+  // (the grid's second axis has 65,535 tiles at most, its first a number of workgroups of 31 bits)
+  if (rows > 65535 * 128ll || cols > 0x7fffffff || ceil_div(cols, 128) * rows > 16 * 0x7fffffffll)
+    return net_fail(BBO_UNSUPPORTED, "matrix too large");
+  if (!q != !scales || !qt != !t_scales) return net_fail(BBO_INVALID_ARG, "values and scales go together");
+  if (rows == 0 || cols == 0 || (!q && !qt)) return BBO_OK;
+  if (!x) return net_fail(BBO_INVALID_ARG, "x is null");
+  if (x_stride < cols || (gate && gate_stride < cols) || (q && (q_stride < cols || scale_stride < ceil_div(cols, 128))) ||
+      (qt && (qt_stride < rows || t_scale_stride < ceil_div(rows, 128))))
+    return net_fail(BBO_INVALID_ARG, "a stride is less than a row");
+  const QuantArgs a{x, gate, (uint8_t*)q, (uint8_t*)scales, (uint8_t*)qt, (uint8_t*)t_scales, x_stride, gate_stride, q_stride,
+                    scale_stride, qt_stride, t_scale_stride, rows, cols};
+  if (dtype == BBO_F32) launch<float>(a, tile, (hipStream_t)stream);
+  else launch<bf16>(a, tile, (hipStream_t)stream);
+  return net_launched();
+}

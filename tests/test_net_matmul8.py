@@ -1,0 +1,172 @@
+"""GPU tests of the 8-bit product against 64 bits."""
+import numpy as np
+import pytest
+import torch
+
+import net_oracle as O
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def net():
+    from paper_2012_04201_amd import net
+    net.lib()
+    return net
+
+
+def matrix(net, rows, cols, tile, seed, pad=True, scales=(100, 140)):
+    """Random codes and scales, with NaN where nothing is to be read."""
+    g = torch.Generator().manual_seed(seed)
+    b = net.empty_blocks8(rows, cols, tile)
+    if not pad:  # dense rows, at odd addresses for odd lengths
+        kb = -(-cols // 128)
+        b = net.Blocks8(torch.empty(rows, cols, dtype=torch.uint8).cuda().view(torch.float8_e4m3fn),
+                        torch.empty(-(-rows // tile), kb, dtype=torch.uint8).cuda().view(torch.float8_e8m0fnu), tile)
+    elif rows:
+        b.values.view(torch.uint8).as_strided((rows, b.values.stride(0)), (b.values.stride(0), 1)).fill_(0x7f)
+        b.scales.view(torch.uint8).as_strided((b.scales.shape[0], b.scales.stride(0)), (b.scales.stride(0), 1)).fill_(255)
+    codes = torch.randint(0, 127, (rows, cols), generator=g) | (torch.randint(0, 2, (rows, cols), generator=g) << 7)
+    b.values.view(torch.uint8).copy_(codes.to(torch.uint8))
+    b.scales.view(torch.uint8).copy_(torch.randint(*scales, tuple(b.scales.shape), generator=g).to(torch.uint8))
+    return b
+
+
+def check(got, a, b, c0=None):
+    A, B = O.values(a), O.values(b)
+    want, size = A @ B.t(), A.abs() @ B.abs().t()
+    if c0 is not None:
+        want, size = want + c0.cpu().double(), size + c0.cpu().double().abs()
+    half = O.EPS16 if got.dtype == torch.bfloat16 else O.EPS32
+    # any order of k float32 additions: (k + 8) half-ulps of the magnitudes' sum; one more rounding.  For bfloat16 each of
+    # eight neighbouring products may lose what it has below 2^-13 of the largest of them: seven times that.
+    bound = size * ((A.shape[1] + 8) * O.EPS32 + (7 * 2.0 ** -13 if got.dtype == torch.bfloat16 else 0)) + want.abs() * half * (1 + 2 ** -7)
+    assert got.shape == want.shape
+    bad = (got.cpu().double() - want).abs() > bound
+    assert not bad.any(), (int(bad.sum()), float(((got.cpu().double() - want).abs() / bound.clamp(min=1e-300)).max()))
+
+
+SHAPES = [(1, 1, 1), (1, 16, 128), (1, 1000, 513), (2, 17, 100), (16, 33, 640), (17, 129, 130), (31, 40, 64), (33, 50, 1), (64, 64, 127), (65, 64, 128),
+          (100, 70, 129), (128, 256, 256), (130, 300, 569), (257, 255, 384), (300, 513, 1000), (1, 300, 5000), (63, 10, 2049)]
+
+
+@pytest.mark.parametrize("m,n,k", SHAPES)
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("tiles", [(1, 1), (1, 128), (128, 1)])
+def test_product(net, m, n, k, dtype, tiles):
+    a, b = matrix(net, m, k, tiles[0], 1), matrix(net, n, k, tiles[1], 2)
+    check(net.matmul8(a, b, dtype=dtype), a, b)
+    c0 = (torch.randn(m, n, generator=torch.Generator().manual_seed(3)) * 10).to(dtype).cuda()
+    check(net.matmul8(a, b, out=c0.clone(), accumulate=True), a, b, c0)
+
+
+@pytest.mark.parametrize("m,n,k", [(1, 50, 301), (20, 70, 129), (150, 90, 333), (260, 130, 257)])
+def test_rows_at_any_address(net, m, n, k):
+    a, b = matrix(net, m, k, 1, 4, pad=False), matrix(net, n, k, 1, 5, pad=False)
+    check(net.matmul8(a, b, dtype=torch.float32), a, b)
+    wide = torch.full((m, n + 7), 3.0).cuda()
+    net.matmul8(a, b, out=wide[:, 3:3 + n])
+    check(wide[:, 3:3 + n], a, b)
+    assert (wide[:, :3] == 3).all() and (wide[:, 3 + n:] == 3).all()
+    wide = torch.full((m, n + 7), 3.0, dtype=torch.bfloat16).cuda()
+    net.matmul8(a, b, out=wide[:, 1:1 + n])
+    check(wide[:, 1:1 + n], a, b)
+    assert (wide[:, :1] == 3).all() and (wide[:, 1 + n:] == 3).all()
+
+
+@pytest.mark.parametrize("m,n,k", [(3300, 4000, 300), (2500, 2300, 200), (1000, 3100, 1024)])
+def test_many_tiles(net, m, n, k):
+    """Larger tiles than the small shapes get, ragged at every edge."""
+    a, b = matrix(net, m, k, 1, 6), matrix(net, n, k, 128, 7)
+    check(net.matmul8(a, b, dtype=torch.float32), a, b)
+    check(net.matmul8(a, b), a, b)
+    a, b = matrix(net, m, k, 1, 6, pad=False), matrix(net, n, k, 1, 7, pad=False)
+    check(net.matmul8(a, b, dtype=torch.float32), a, b)
+
+
+@pytest.mark.parametrize("m", [1, 40, 200])
+def test_scales_from_one_end_to_the_other(net, m):
+    """Scales down to 2^-127 and up to 2^100, zeros under the largest, and NaN as value and as scale."""
+    n, k = 96, 512
+    a, b = matrix(net, m, k, 1, 8, scales=(0, 30)), matrix(net, n, k, 1, 9, scales=(210, 227))
+    check(net.matmul8(a, b, dtype=torch.float32), a, b)
+    a, b = matrix(net, m, k, 1, 10), matrix(net, n, k, 1, 11)
+    a.values.view(torch.uint8)[0, 200] = 0x7f
+    b.scales.view(torch.uint8)[5, 3] = 255
+    got = net.matmul8(a, b, dtype=torch.float32).cpu()
+    nan = torch.zeros(m, n, dtype=torch.bool)
+    nan[0], nan[:, 5] = True, True
+    assert torch.equal(got.isnan(), nan)
+
+
+def test_nothing_contracted(net):
+    a, b = net.empty_blocks8(5, 0), net.empty_blocks8(70, 0)
+    assert (net.matmul8(a, b) == 0).all()
+    c = torch.ones(5, 70).cuda()
+    assert (net.matmul8(a, b, out=c, accumulate=True) == 1).all()
+    a, b = net.empty_blocks8(300, 0), net.empty_blocks8(70, 0)
+    assert (net.matmul8(a, b) == 0).all()
+    assert net.matmul8(net.empty_blocks8(0, 50), net.empty_blocks8(3, 50)).shape == (0, 3)
+
+
+def test_a_layers_gradients(net):
+    """y = x w^T in 8 bits: dx and dw are the products of the 8-bit gradient, which differences of y agree with."""
+    g = torch.Generator().manual_seed(12)
+    m, n, k = 210, 140, 330
+    x, w, dy = torch.randn(m, k, generator=g), torch.randn(n, k, generator=g) * k ** -0.5, torch.randn(m, n, generator=g) * 1e-3
+    x8, x8t = net.quantize(x.cuda(), want_cols=True)
+    w8, w8t = net.quantize(w.cuda(), tile=128, want_cols=True)
+    d8, d8t = net.quantize(dy.cuda(), want_cols=True)
+    y, dx, dw = net.matmul8(x8, w8, torch.float32), net.matmul8(d8, w8t, torch.float32), net.matmul8(d8t, x8t, torch.float32)
+    check(y, x8, w8)
+    check(dx, d8, w8t)
+    check(dw, d8t, x8t)
+    X, W, D = x.double(), O.values(w8), O.values(d8)
+    v = torch.randn(m, k, generator=g, dtype=torch.float64)
+    slope = float((D * ((X + v) @ W.t() - X @ W.t())).sum())  # y is linear in x and in w
+    dot = dx.cpu().double() * v
+    assert abs(slope - float(dot.sum())) <= 1e-5 * float(dot.abs().sum())
+    Dt, Xt = O.values(d8t), O.values(x8t)
+    u = torch.randn(n, k, generator=g, dtype=torch.float64)
+    slope = float((Dt.t() * (Xt.t() @ u.t())).sum())
+    dot = dw.cpu().double() * u
+    assert abs(slope - float(dot.sum())) <= 1e-5 * float(dot.abs().sum())
+
+
+def test_accuracy_on_normal_data(net):
+    """Relative to the result: float32's rounding of a sum of 1000, and 3e-5 beside the bfloat16 output's rounding of 2^-8 / sqrt(12) to sqrt(3)."""
+    g = torch.Generator().manual_seed(17)
+    for m in (4, 200):
+        a, b = (net.quantize(torch.randn(n, 1000, generator=g).cuda())[0] for n in (m, 300))
+        want = O.values(a) @ O.values(b).t()
+        assert float((net.matmul8(a, b, dtype=torch.float32).cpu().double() - want).norm() / want.norm()) < 1e-6
+        got = net.matmul8(a, b).cpu()
+        away = (got.double() - want).abs() > (want.bfloat16().double() - want).abs() + 1e-3 * want.abs()
+        assert float(away.double().mean()) < 0.02  # rounded the other way than the exact result would be
+
+
+def test_the_same_call_gives_the_same_bits(net):
+    for m, n, k in ((3, 200, 4000), (100, 100, 4000), (500, 600, 700)):
+        a, b = matrix(net, m, k, 1, 13), matrix(net, n, k, 1, 14)
+        first = net.matmul8(a, b, dtype=torch.float32)
+        assert all(torch.equal(first, net.matmul8(a, b, dtype=torch.float32)) for _ in range(3))
+
+
+def test_another_stream_and_a_graph(net):
+    for m, n, k in ((2, 300, 3000), (200, 300, 600)):
+        a, b = matrix(net, m, k, 1, 15), matrix(net, n, k, 1, 16)
+        want = net.matmul8(a, b)
+        torch.cuda.synchronize()
+        side = torch.cuda.Stream()
+        got = net.matmul8(a, b, stream=side)
+        side.synchronize()
+        assert torch.equal(got, want)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            out = net.matmul8(a, b)
+        for i in range(3):
+            b.scales.view(torch.uint8).copy_(b.scales.view(torch.uint8).roll(i, 0))
+            graph.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(out.clone(), net.matmul8(a, b))
+            torch.cuda.synchronize()

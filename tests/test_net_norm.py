@@ -1,0 +1,198 @@
+"""GPU tests of the norm and its gradient against 64 bits."""
+import numpy as np
+import pytest
+import torch
+
+import net_oracle as O
+
+pytestmark = pytest.mark.gpu
+EPS = 1e-6
+# A row of n squares: a thread adds at most 32, a row's 1024 threads join in at most 20 more steps, and each square is rounded:
+# 64 half-ulps bound the mean's relative error, half of that rstd's; two more products and the reciprocal root (1 ulp).
+Y_TOL = 40 * O.EPS32
+
+
+@pytest.fixture(scope="module")
+def net():
+    from paper_2012_04201_amd import net
+    net.lib()
+    return net
+
+
+def data(rows, width, dtype, seed=0):
+    g = torch.Generator().manual_seed(1000 * rows + width + seed)
+    r = lambda *n: torch.randn(*n, generator=g)
+    x = (r(rows, width) * (r(width) * 0.7).exp()).to(dtype)
+    return x, (r(rows, width) * 0.5).to(dtype), 1 + 0.1 * r(width), (r(rows, width) * 1e-2).to(dtype), (r(rows, width) * 1e-2).to(dtype)
+
+
+def half_ulp(dtype):
+    return O.EPS16 if dtype == torch.bfloat16 else O.EPS32
+
+
+def check(got, want, bound):
+    got = got.cpu().double()
+    assert got.shape == want.shape
+    bad = (got - want).abs() > bound
+    assert not bad.any(), (int(bad.sum()), float(((got - want).abs() / bound.clamp(min=1e-300)).max()))
+
+
+def check_y8(b, y):
+    """Each value within half a step of e4m3 at y, with the scale that y's largest asks for (both up to the arithmetic before the rounding)."""
+    raw = b.scales.cpu().contiguous().view(torch.uint8).double()
+    s = torch.exp2(raw - 127)
+    pad = torch.nn.functional.pad(y.abs(), (0, -y.shape[1] % 128)).view(y.shape[0], -1, 128).amax(2)
+    assert (pad <= 448 * s * (1 + Y_TOL)).all() and ((pad > 224 * s * (1 - Y_TOL)) | (raw == 0)).all()
+    sv = s.repeat_interleave(128, 1)[:, :y.shape[1]]
+    check(O.values(b), y, y.abs() * (2.0 ** -4 + Y_TOL) + sv * 2.0 ** -10)
+
+
+SHAPES = [(1, 1), (3, 7), (1, 1024), (5, 129), (33, 512), (70, 513), (17, 1024), (9, 1111), (6, 2048), (5, 2049), (4, 4099), (3, 8192), (3, 8193),
+          (2, 16384), (2, 20001), (1, 32768)]
+
+
+@pytest.mark.parametrize("rows,width", SHAPES)
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("residual", [False, True])
+def test_norm(net, rows, width, dtype, residual):
+    x, r, w, _, _ = data(rows, width, dtype)
+    f = net.rms_norm(x.cuda(), w.cuda(), residual=r.cuda() if residual else None, eps=EPS, want_rstd=True, want_8bit=True)
+    h = x
+    if residual:
+        h = (x.float() + r.float()).to(dtype)
+        assert torch.equal(f.sum.cpu(), h)
+    else:
+        assert f.sum is None
+    y = O.rms_norm(h.double(), w.double(), EPS)
+    check(f.y, y, y.abs() * (half_ulp(dtype) * (1 + 2 ** -7) + Y_TOL))
+    rstd = (h.double().square().mean(1) + EPS).rsqrt()
+    check(f.rstd, rstd, rstd * Y_TOL)
+    check_y8(f.y8, y)
+    g = net.rms_norm(x.cuda(), None, residual=r.cuda() if residual else None, eps=EPS, want_y=False, want_8bit=True)
+    assert g.y is None and g.rstd is None
+    check_y8(g.y8, O.rms_norm(h.double(), torch.ones(width).double(), EPS))
+
+
+@pytest.mark.parametrize("rows,width", SHAPES + [(700, 100), (3000, 70)])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("dsum", [False, True])
+def test_gradient(net, rows, width, dtype, dsum):
+    h, _, w, dy, ds = data(rows, width, dtype, 1)
+    rstd32 = (h.double().square().mean(1) + EPS).rsqrt().float()
+    dx, dw = net.rms_norm_grad(dy.cuda(), h.cuda(), rstd32.cuda(), w.cuda(), dsum=ds.cuda() if dsum else None)
+    rstd, H, W, D = rstd32.double()[:, None], h.double(), w.double(), dy.double()
+    xh = H * rstd
+    g = D * W
+    want = rstd * (g - xh * (g * xh).mean(1, keepdim=True)) + (ds.double() if dsum else 0)
+    # the mean as in Y_TOL, of magnitudes; then products and sums of the three terms
+    size = rstd * (g.abs() + xh.abs() * (g * xh).abs().mean(1, keepdim=True)) + (ds.double().abs() if dsum else 0)
+    check(dx, want, size * 80 * O.EPS32 + want.abs() * half_ulp(dtype) * (1 + 2 ** -7))
+    # a share of the sum has at most rows additions, the shares are joined in at most 128 + 16 more
+    check(dw, (D * xh).sum(0), (D * xh).abs().sum(0) * (rows + 150) * O.EPS32)
+    assert net.rms_norm_grad(dy.cuda(), h.cuda(), rstd32.cuda(), w.cuda(), want_dweight=False)[1] is None
+
+
+def test_gradient_against_differences(net):
+    """Of sum(c * y) + sum(e * h) with h = x + r, in 64 bits, along random directions."""
+    rows, width = 6, 333
+    x, r, w, c, e = (t.double() for t in data(rows, width, torch.float32, 2))
+    f = net.rms_norm(x.float().cuda(), w.float().cuda(), residual=r.float().cuda(), eps=EPS, want_rstd=True)
+    dx, dw = net.rms_norm_grad(c.float().cuda(), f.sum, f.rstd, w.float().cuda(), dsum=e.float().cuda())
+    x, r, w, c, e = (t.float().double() for t in (x, r, w, c, e))
+    loss = lambda x, r, w: float((c * O.rms_norm(x + r, w, EPS)).sum() + (e * (x + r)).sum())
+    gen = torch.Generator().manual_seed(3)
+    for which, grad in ((0, dx), (1, dx), (2, dw)):
+        d = torch.randn((x, r, w)[which].shape, generator=gen, dtype=torch.float64)
+        t = 1e-5
+        args = [[x, r, w], [x, r, w]]
+        args[0][which], args[1][which] = args[0][which] + t * d, args[1][which] - t * d
+        slope = (loss(*args[0]) - loss(*args[1])) / (2 * t)
+        dot = grad.cpu().double() * d
+        # the differences' error is of the order t^2 and 1e-16 / t; float32's by the sizes of the terms
+        assert abs(slope - float(dot.sum())) <= 1e-6 * float(dot.abs().sum())
+
+
+def test_strides_and_alignment(net):
+    """Rows with gaps and at odd addresses, the sum in place of the residual stream."""
+    rows, width = 21, 777
+    for dtype in (torch.float32, torch.bfloat16):
+        x, r, w, dy, ds = data(rows, width, dtype, 4)
+        wide = lambda t, off, gap: torch.full((rows, width + gap), 99.0, dtype=dtype).cuda()[:, off:off + width].copy_(t)
+        xs, rs, dys, dss = wide(x, 1, 5), wide(r, 3, 3), wide(dy, 2, 9), wide(ds, 1, 1)
+        a = net.rms_norm(xs, w.cuda(), residual=rs, eps=EPS, want_rstd=True, want_8bit=True)
+        b = net.rms_norm(x.cuda(), w.cuda(), residual=r.cuda(), eps=EPS, want_rstd=True, want_8bit=True)
+        assert torch.equal(a.y, b.y) and torch.equal(a.sum, b.sum) and torch.equal(a.rstd, b.rstd)
+        assert torch.equal(O.values(a.y8), O.values(b.y8))
+        ga = net.rms_norm_grad(dys, wide(b.sum.cpu(), 1, 3), a.rstd, w.cuda(), dsum=dss)
+        gb = net.rms_norm_grad(dy.cuda(), b.sum, b.rstd, w.cuda(), dsum=ds.cuda())
+        assert torch.equal(ga[0], gb[0]) and torch.equal(ga[1], gb[1])
+        # outputs over the inputs that may be
+        L, p = net.lib(), lambda t: t.data_ptr()
+        x2, dy2, wd = x.cuda(), dy.cuda(), w.cuda()
+        r2 = r.cuda()
+        st = torch.cuda.current_stream().cuda_stream
+        dt = net._DTYPES[dtype]
+        assert L.bbo_net_rms_norm(p(x2), width, p(r2), width, p(wd), rows, width, EPS, dt, p(r2), width, 0, 0, 0, 0, 0, 0, 0, st) == 0
+        assert torch.equal(r2, b.sum)
+        assert L.bbo_net_rms_norm_grad(p(dy2), width, p(dss), dss.stride(0), p(b.sum), width, p(b.rstd), p(wd), rows, width, dt, p(dy2), width, 0, 0, 0, st) == 0
+        assert torch.equal(dy2, gb[0])
+        # nothing is written between the rows
+        guard = torch.full((rows, width + 8), 7.0, dtype=dtype).cuda()
+        assert L.bbo_net_rms_norm(p(x2), width, 0, 0, p(wd), rows, width, EPS, dt, 0, 0, p(guard) + 3 * guard.element_size(), width + 8, 0, 0, 0, 0, 0, st) == 0
+        assert (guard[:, :3] == 7).all() and (guard[:, 3 + width:] == 7).all()
+
+
+def test_rows_that_hold_nothing_or_too_much(net):
+    width = 300
+    x = torch.randn(6, width, generator=torch.Generator().manual_seed(1))
+    x[0] = 0
+    x[1, 5] = float("inf")
+    x[2, 7] = float("nan")
+    x[3] = 3e38
+    x[4] = 1e-30
+    w = torch.ones(width)
+    f = net.rms_norm(x.cuda(), w.cuda(), eps=EPS, want_rstd=True, want_8bit=True)
+    y, v = f.y.cpu(), O.values(f.y8)
+    assert (y[0] == 0).all() and (v[0] == 0).all()
+    one = torch.zeros(width, dtype=torch.bool)
+    one[5] = True
+    assert torch.equal(y[1].isnan(), one) and torch.equal(v[1].isnan(), one) and (y[1][~one] == 0).all()
+    assert y[2].isnan().all() and v[2].isnan().all()
+    assert (y[3] == 0).all()  # its squares pass float32's range
+    check(f.y[4:5], O.rms_norm(x[4:5].double(), w.double(), EPS), torch.full((1, width), 1e-33).double())
+    assert torch.isfinite(y[5]).all() and torch.isfinite(v[5]).all()
+    z = net.rms_norm(torch.zeros(2, 4).cuda(), None, eps=0.0).y  # 0 * inf, as the formula says
+    assert z.isnan().all()
+
+
+def test_no_rows(net):
+    x = torch.zeros(0, 50).cuda()
+    f = net.rms_norm(x, None, residual=x, want_rstd=True, want_8bit=True)
+    assert f.y.shape == f.sum.shape == (0, 50) and f.rstd.shape == (0,)
+    dx, dw = net.rms_norm_grad(x, x, f.rstd)
+    assert dx.shape == (0, 50) and (dw == 0).all() and dw.shape == (50,)
+
+
+def test_another_stream_and_a_graph(net):
+    x, r, w, dy, ds = (t.cuda() for t in data(65, 1000, torch.bfloat16, 6))
+
+    def step(stream=None):
+        f = net.rms_norm(x, w, residual=r, eps=EPS, want_rstd=True, want_8bit=True, stream=stream)
+        return (f.y, f.sum, f.y8.values.view(torch.uint8), f.y8.scales.view(torch.uint8)) + net.rms_norm_grad(dy, f.sum, f.rstd, w, dsum=ds, stream=stream)
+
+    want = [t.clone() for t in step()]
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    got = step(side)
+    side.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = step()
+    for k in range(3):
+        x.copy_(x.roll(k, 0))
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in out]
+        assert all(torch.equal(a, b) for a, b in zip(got, step()))
+        torch.cuda.synchronize()
