@@ -148,12 +148,15 @@ __device__ inline void block_products(f32x4 (&acc)[MI][NI], const int (&sa)[MI],
   }
 }
 
-// Four scales of a row from block kb on, those past the row's end as 127; block kb + i in bits 8 i.
-__device__ inline uint32_t load_scales(const uint8_t* row, int64_t kb, int64_t blocks) {
+// Four scales of a row from block kb < blocks on, block kb + i in bits 8 i; 0 past the row's end.
+__device__ inline uint32_t load_scales(const uint8_t* row, int kb, int blocks) {
   typedef uint32_t u32_any __attribute__((aligned(1)));
-  if (kb + 4 <= blocks) return *(const u32_any*)(row + kb);
-  uint32_t v = 0x7f7f7f7f;
-  for (int i = 0; kb + i < blocks; i++) v = (v & ~(255u << (8 * i))) | (uint32_t)row[kb + i] << (8 * i);
+  if (blocks >= 4) {  // (the last four, shifted, where fewer than four follow)
+    const int at = kb + 4 <= blocks ? kb : blocks - 4;
+    return *(const u32_any*)(row + at) >> (8 * (kb - at));
+  }
+  uint32_t v = 0;
+  for (int i = 0; kb + i < blocks; i++) v |= (uint32_t)row[kb + i] << (8 * i);
   return v;
 }
 
@@ -209,91 +212,101 @@ __global__ __launch_bounds__(64 * W) void k_mm_rows(const MatArgs g) {
 // ---------------------------------------------------------------------------
 __device__ inline int mix(int row) { return (row & 7) ^ (row >> 3 & 1); }
 
-template <bool EXACT, int BM, int BN, int WM, int WN>
-__global__ __launch_bounds__(64 * WM * WN) void k_mm_tile(const MatArgs g, int tiles_m, int tiles_n) {
-  constexpr int W = WM * WN, MI = BM / WM / 16, NI = BN / WN / 16;
-  __shared__ __attribute__((aligned(128))) uint8_t lds[2][(BM + BN) * 128];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r16 = lane & 15, q = lane >> 4;
-  const int wm = wave / WN, wn = wave % WN;
-  const int tile_m = blockIdx.x % tiles_m, tile_n = blockIdx.x / tiles_m;
-  const int64_t m0 = (int64_t)tile_m * BM, n0 = (int64_t)tile_n * BN;
-  const int64_t blocks = ceil_div_d(g.k, 128), direct = g.direct ? g.k >> 7 : 0;
+// The tile of a workgroup.  Workgroups go round the eight XCDs in turn, so that those of one XCD get a run of tiles of its own;
+// a run goes down bands of eight tiles' rows, whose operands its L2 holds.
+__device__ inline void tile_of(int tiles_m, int tiles_n, int& tm, int& tn) {
+  const int count = tiles_m * tiles_n, id = blockIdx.x, per = count >> 3, rest = count & 7, x = id & 7;
+  const int t = x * per + (x < rest ? x : rest) + (id >> 3);
+  const int band = t / (8 * tiles_n), at = t - band * 8 * tiles_n;
+  const int high = tiles_m - band * 8 < 8 ? tiles_m - band * 8 : 8;
+  tm = band * 8 + at % high;
+  tn = at / high;
+}
 
-  // Rows of the two operands, one after the other: [0, BM) of a, [BM, BM + BN) of b; those past the end repeat the last.
-  auto row_of = [&](int r) -> const uint8_t* {
-    if (r < BM) {
-      const int64_t m = m0 + r < g.m ? m0 + r : g.m - 1;
-      return g.a + m * g.a_stride;
-    }
-    const int64_t n = n0 + r - BM < g.n ? n0 + r - BM : g.n - 1;
-    return g.b + n * g.b_stride;
-  };
-  constexpr int LOADS = (BM + BN) / 8 / W;  // of 8 rows each by a wave
-  const uint8_t* from[LOADS];
+template <bool EXACT, int BM, int BN, int WM, int WN, int PER_CU>
+__global__ __launch_bounds__(64 * WM * WN, WM * WN * PER_CU / 4) void k_mm_tile(const MatArgs g, int tiles_m, int tiles_n) {
+  constexpr int W = WM * WN, MI = BM / WM / 16, NI = BN / WN / 16;
+  constexpr int LA = BM / 8 / W, LB = BN / 8 / W;  // loads of 8 rows each by a wave
+  static_assert(BM + BN <= 64 * W, "a thread for each row's scales");
+  __shared__ __attribute__((aligned(128))) uint8_t lds[2][(BM + BN) * 128];
+  __shared__ uint32_t four[2][BM + BN];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r16 = lane & 15, q = lane >> 4;
+  const int wm = wave / WN * (BM / WM), wn = wave % WN * (BN / WN);
+  int tile_m, tile_n;
+  tile_of(tiles_m, tiles_n, tile_m, tile_n);
+  const int64_t m0 = (int64_t)tile_m * BM, n0 = (int64_t)tile_n * BN;
+  const int rows_a = (int)(g.m - m0 < BM ? g.m - m0 : BM) - 1, rows_b = (int)(g.n - n0 < BN ? g.n - n0 : BN) - 1;  // the last ones
+  const int blocks = (int)ceil_div_d(g.k, 128), direct = g.direct ? (int)(g.k >> 7) : 0;
+  const uint8_t* const a0 = g.a + m0 * g.a_stride;
+  const uint8_t* const b0 = g.b + n0 * g.b_stride;
+
+  // A lane's piece of row r: rows past the operand's end repeat the last.  (Offsets in a tile have 32 bits: the host sees to it.)
+  const int piece = ((lane & 7) ^ mix((wave & 1) * 8 + (lane >> 3))) * 16;  // (a wave's rows start at multiples of 8: the same f for all its loads)
+  uint32_t from_a[LA], from_b[LB];
 #pragma unroll
-  for (int j = 0; j < LOADS; j++) {
-    const int r = (j * W + wave) * 8 + (lane >> 3);
-    from[j] = row_of(r) + ((lane & 7) ^ mix(r)) * 16;
-  }
-  auto stage = [&](int64_t kb, int to) {
+  for (int j = 0; j < LA; j++) from_a[j] = (uint32_t)(min((j * W + wave) * 8 + (lane >> 3), rows_a)) * (uint32_t)g.a_stride + piece;
 #pragma unroll
-    for (int j = 0; j < LOADS; j++)
-      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(from[j] + kb * 128),
+  for (int j = 0; j < LB; j++) from_b[j] = (uint32_t)(min((j * W + wave) * 8 + (lane >> 3), rows_b)) * (uint32_t)g.b_stride + piece;
+  auto stage = [&](int kb, int to) {
+    const uint8_t *pa = a0 + (int64_t)kb * 128, *pb = b0 + (int64_t)kb * 128;
+#pragma unroll
+    for (int j = 0; j < LA; j++)
+      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(pa + from_a[j]),
                                        (__attribute__((address_space(3))) void*)&lds[to][(j * W + wave) * 1024], 16, 0, 0);
+#pragma unroll
+    for (int j = 0; j < LB; j++)
+      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(pb + from_b[j]),
+                                       (__attribute__((address_space(3))) void*)&lds[to][BM * 128 + (j * W + wave) * 1024], 16, 0, 0);
   };
-  const uint8_t *as[MI], *bs[NI];
-  uint32_t sa4[MI], sb4[NI], sa_next[MI], sb_next[NI];
-#pragma unroll
-  for (int i = 0; i < MI; i++) {
-    const int64_t m = m0 + wm * (BM / WM) + i * 16 + r16;
-    as[i] = g.as + ((m < g.m ? m : g.m - 1) >> g.a_shift) * g.as_stride;
-    sa_next[i] = sa4[i] = load_scales(as[i], 0, blocks);
-  }
-#pragma unroll
-  for (int i = 0; i < NI; i++) {
-    const int64_t n = n0 + wn * (BN / WN) + i * 16 + r16;
-    bs[i] = g.bs + ((n < g.n ? n : g.n - 1) >> g.b_shift) * g.bs_stride;
-    sb_next[i] = sb4[i] = load_scales(bs[i], 0, blocks);
-  }
+  // Scales: a thread has one of the tile's rows, asks for those of four blocks four blocks ahead and leaves them in LDS.
+  const bool has_row = tid < BM + BN;
+  const uint8_t* const scales = tid < BM ? g.as + ((m0 + min(tid, rows_a)) >> g.a_shift) * g.as_stride
+                                         : g.bs + ((n0 + min(tid - BM, rows_b)) >> g.b_shift) * g.bs_stride;
+  uint32_t next = 0;
+  auto ask_scales = [&](int kb) {
+    if (has_row && kb < blocks) next = load_scales(scales, kb, blocks);
+  };
+  auto keep_scales = [&](int kb) {  // of the four blocks from kb on
+    if (has_row) four[kb >> 2 & 1][tid] = next;
+  };
   f32x4 acc[MI][NI] = {};
   const int p0 = (q * 2 ^ mix(r16)) * 16, p1 = ((q * 2 + 1) ^ mix(r16)) * 16;
-  auto products = [&](int64_t kb, int in) {
+  auto products = [&](int kb, int in) {
     auto frag = [&](int row16) {
       const uint8_t* at = &lds[in][(row16 + r16) * 128];
       const i32x4 lo = *(const i32x4*)(at + p0), hi = *(const i32x4*)(at + p1);
       return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
     };
-    const int shift = (int)(kb & 3) * 8;
+    const uint8_t* s = (const uint8_t*)&four[kb >> 2 & 1][r16] + (kb & 3);
     int sa[MI], sb[NI];
 #pragma unroll
-    for (int i = 0; i < MI; i++) sa[i] = sa4[i] >> shift & 255;
+    for (int i = 0; i < MI; i++) sa[i] = s[(wm + i * 16) * 4];
 #pragma unroll
-    for (int i = 0; i < NI; i++) sb[i] = sb4[i] >> shift & 255;
-    block_products<EXACT, MI, NI>(acc, sa, sb, [&](int i) { return frag(wm * (BM / WM) + i * 16); },
-                                  [&](int j) { return frag(BM + wn * (BN / WN) + j * 16); });
+    for (int i = 0; i < NI; i++) sb[i] = s[(BM + wn + i * 16) * 4];
+    block_products<EXACT, MI, NI>(acc, sa, sb, [&](int i) { return frag(wm + i * 16); }, [&](int j) { return frag(BM + wn + j * 16); });
   };
-  // The scales of the four blocks from kb on; asked for four blocks ahead.
-  auto next_scales = [&](int64_t kb) {
-    if ((kb & 3) == 0) {
-#pragma unroll
-      for (int i = 0; i < MI; i++) sa4[i] = sa_next[i], sa_next[i] = load_scales(as[i], kb + 4, blocks);
-#pragma unroll
-      for (int i = 0; i < NI; i++) sb4[i] = sb_next[i], sb_next[i] = load_scales(bs[i], kb + 4, blocks);
-    }
+  // (block kb's scales were kept in block kb - 1 or before; what block kb - 1 read is free)
+  auto next_scales = [&](int kb) {
+    if ((kb & 3) == 0) ask_scales(kb + 4);
+    if ((kb & 3) == 3) keep_scales(kb + 1);
   };
+  ask_scales(0);
+  keep_scales(0);
   if (direct > 0) stage(0, 0);
-  for (int64_t kb = 0; kb < direct; kb++) {
+  for (int kb = 0; kb < direct; kb++) {
     __syncthreads();  // this block has landed, and the other half is free
     next_scales(kb);
-    if (kb + 1 < direct) stage(kb + 1, (int)(kb + 1) & 1);
-    products(kb, (int)kb & 1);
+    if (kb + 1 < direct) stage(kb + 1, (kb + 1) & 1);
+    products(kb, kb & 1);
   }
-  for (int64_t kb = direct; kb < blocks; kb++) {
+  for (int kb = direct; kb < blocks; kb++) {
     __syncthreads();
-    for (int j = 0; j < LOADS; j++) {
-      const int r = (j * W + wave) * 8 + (lane >> 3);
-      *(i32x4*)&lds[0][(j * W + wave) * 1024 + lane * 16] = load16(row_of(r), kb * 128 + ((lane & 7) ^ mix(r)) * 16, g.k);
-    }
+    for (int j = 0; j < LA; j++)
+      *(i32x4*)&lds[0][(j * W + wave) * 1024 + lane * 16] =
+          load16(a0 + (int64_t)min((j * W + wave) * 8 + (lane >> 3), rows_a) * g.a_stride, (int64_t)kb * 128 + piece, g.k);
+    for (int j = 0; j < LB; j++)
+      *(i32x4*)&lds[0][BM * 128 + (j * W + wave) * 1024 + lane * 16] =
+          load16(b0 + (int64_t)min((j * W + wave) * 8 + (lane >> 3), rows_b) * g.b_stride, (int64_t)kb * 128 + piece, g.k);
     next_scales(kb);
     __syncthreads();
     products(kb, 0);
@@ -301,27 +314,27 @@ __global__ __launch_bounds__(64 * WM * WN) void k_mm_tile(const MatArgs g, int t
 #pragma unroll
   for (int i = 0; i < MI; i++)
 #pragma unroll
-    for (int j = 0; j < NI; j++)
-      put4(g, m0 + wm * (BM / WM) + i * 16 + r16, n0 + wn * (BN / WN) + j * 16 + q * 4, acc[i][j]);
+    for (int j = 0; j < NI; j++) put4(g, m0 + wm + i * 16 + r16, n0 + wn + j * 16 + q * 4, acc[i][j]);
 }
 
 template <bool EXACT, int MT>
 void rows(const MatArgs& g, hipStream_t s) {
   hipLaunchKernelGGL((k_mm_rows<EXACT, MT, 8>), dim3((uint32_t)ceil_div(g.n, 16)), dim3(512), 0, s, g);
 }
-template <bool EXACT, int BM, int BN, int WM, int WN>
+template <bool EXACT, int BM, int BN, int WM, int WN, int PER_CU>
 void tiles(const MatArgs& g, hipStream_t s) {
   const int tm = (int)ceil_div(g.m, BM), tn = (int)ceil_div(g.n, BN);
-  hipLaunchKernelGGL((k_mm_tile<EXACT, BM, BN, WM, WN>), dim3((uint32_t)((int64_t)tm * tn)), dim3(64 * WM * WN), 0, s, g, tm, tn);
+  hipLaunchKernelGGL((k_mm_tile<EXACT, BM, BN, WM, WN, PER_CU>), dim3((uint32_t)((int64_t)tm * tn)), dim3(64 * WM * WN), 0, s, g, tm, tn);
 }
 template <bool EXACT>
 void launch(const MatArgs& g, hipStream_t s) {
   if (g.m <= 16) rows<EXACT, 1>(g, s);
   else if (g.m <= 32) rows<EXACT, 2>(g, s);
   else if (g.m <= 64) rows<EXACT, 4>(g, s);
-  else if (ceil_div(g.m, 256) * ceil_div(g.n, 256) >= 192) tiles<EXACT, 256, 256, 2, 4>(g, s);
-  else if (ceil_div(g.m, 128) * ceil_div(g.n, 128) >= 192) tiles<EXACT, 128, 128, 2, 2>(g, s);
-  else tiles<EXACT, 64, 64, 2, 2>(g, s);
+  else if (!EXACT && ceil_div(g.m, 256) * ceil_div(g.n, 256) >= 192) tiles<false, 256, 256, 2, 4, 1>(g, s);
+  else if (EXACT && ceil_div(g.m, 256) * ceil_div(g.n, 128) >= 192) tiles<true, 256, 128, 4, 2, 1>(g, s);
+  else if (ceil_div(g.m, 128) * ceil_div(g.n, 128) >= 192) tiles<EXACT, 128, 128, 2, 2, 2>(g, s);
+  else tiles<EXACT, 64, 64, 2, 2, 2>(g, s);
 }
 
 }  // namespace
@@ -345,7 +358,7 @@ int bbo_net_matmul8(const void* a, int64_t a_stride, const void* a_scales, int64
   if ((a_tile != 1 && a_tile != 128) || (b_tile != 1 && b_tile != 128)) return net_fail(BBO_INVALID_ARG, "tile must be 1 or 128");
   if (!float_type(c_dtype)) return net_fail(BBO_INVALID_ARG, "unknown dtype");
   // (a grid's 31 bits of workgroups, the smallest 16 columns)
-  if (m > (1ll << 31) || n > (1ll << 31) || k > (1ll << 31) || ceil_div(m, 64) * ceil_div(n, 64) > 0x7fffffff)
+  if (m >= (1ll << 31) || n >= (1ll << 31) || k >= (1ll << 31) || ceil_div(m, 64) * ceil_div(n, 64) > 0x7fffffff)
     return net_fail(BBO_UNSUPPORTED, "matrix too large");
   if (m == 0 || n == 0) return BBO_OK;
   if (!c) return net_fail(BBO_INVALID_ARG, "c is null");
@@ -360,7 +373,8 @@ int bbo_net_matmul8(const void* a, int64_t a_stride, const void* a_scales, int64
   const MatArgs g{(const uint8_t*)a, (const uint8_t*)a_scales, (const uint8_t*)b, (const uint8_t*)b_scales, c, a_stride,
                   a_scale_stride, b_stride, b_scale_stride, c_stride, m, n, k, a_tile == 128 ? 7 : 0, b_tile == 128 ? 7 : 0,
                   c_dtype == BBO_F32, accumulate != 0,
-                  !(((uintptr_t)a | (uintptr_t)b | (uint64_t)a_stride | (uint64_t)b_stride) & 15)};
+                  !(((uintptr_t)a | (uintptr_t)b | (uint64_t)a_stride | (uint64_t)b_stride) & 15) && a_stride < (1 << 23) &&
+                      b_stride < (1 << 23)};
   if (g.c_f32) launch<true>(g, (hipStream_t)stream);
   else launch<false>(g, (hipStream_t)stream);
   return net_launched();
