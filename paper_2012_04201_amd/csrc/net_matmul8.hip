@@ -9,6 +9,8 @@
 // and whose products and sums are float32: half the rate, 1e-7.
 //
 // The instructions' first operand is b and the second a: a lane then holds four neighbouring columns of one row of c.
+#include <type_traits>
+
 #include "net_common.h"
 
 namespace {
@@ -22,11 +24,17 @@ struct MatArgs {
   int c_f32, accumulate, direct;
 };
 
+typedef int i32x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
+template <int I>
+using Int = std::integral_constant<int, I>;
+
+// (the scales are bytes SB and SA of theirs)
+template <int SB = 0, int SA = 0>
 __device__ inline f32x4 mfma8(i32x8 b, i32x8 a, f32x4 c, int sb, int sa) {
-  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b, a, c, 0, 0, 0, sb, 0, sa);
+  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b, a, c, 0, 0, SB, sb, SA, sa);
 }
 
 // 32 codes of a row as bfloat16, times a power of two.
@@ -108,11 +116,21 @@ __device__ inline void block_products(f32x4 (&acc)[MI][NI], const int (&sa)[MI],
     i32x8 b[NI];
 #pragma unroll
     for (int j = 0; j < NI; j++) b[j] = get_b(j);
+    i32x8 a[2];
+    a[0] = get_a(0);
 #pragma unroll
     for (int i = 0; i < MI; i++) {
-      const i32x8 a = get_a(i);
+      if (i + 1 < MI) a[(i + 1) & 1] = get_a(i + 1);
 #pragma unroll
-      for (int j = 0; j < NI; j++) acc[i][j] = mfma8(b[j], a, acc[i][j], sb[j], sa[i]);
+      for (int j = 0; j < NI; j++) acc[i][j] = mfma8(b[j], a[i & 1], acc[i][j], sb[j], sa[i]);
+    }
+    if constexpr (MI > 1 && NI > 1) {  // the operand of the next products is on its way while these run
+      __builtin_amdgcn_sched_group_barrier(0x100, MI + NI + 2 * NI + 2, 0);
+#pragma unroll
+      for (int i = 0; i < MI; i++) {
+        if (i + 1 < MI) __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+        __builtin_amdgcn_sched_group_barrier(0x8, NI, 0);
+      }
     }
   } else {
     bool ok = true;
@@ -148,9 +166,10 @@ __device__ inline void block_products(f32x4 (&acc)[MI][NI], const int (&sa)[MI],
   }
 }
 
+typedef uint32_t u32_any __attribute__((aligned(1)));
+
 // Four scales of a row from block kb < blocks on, block kb + i in bits 8 i; 0 past the row's end.
 __device__ inline uint32_t load_scales(const uint8_t* row, int kb, int blocks) {
-  typedef uint32_t u32_any __attribute__((aligned(1)));
   if (blocks >= 4) {  // (the last four, shifted, where fewer than four follow)
     const int at = kb + 4 <= blocks ? kb : blocks - 4;
     return *(const u32_any*)(row + at) >> (8 * (kb - at));
@@ -263,11 +282,11 @@ __global__ __launch_bounds__(64 * WM * WN, WM * WN * PER_CU / 4) void k_mm_tile(
   const uint8_t* const scales = tid < BM ? g.as + ((m0 + min(tid, rows_a)) >> g.a_shift) * g.as_stride
                                          : g.bs + ((n0 + min(tid - BM, rows_b)) >> g.b_shift) * g.bs_stride;
   uint32_t next = 0;
-  auto ask_scales = [&](int kb) {
-    if (has_row && kb < blocks) next = load_scales(scales, kb, blocks);
+  auto ask_scales = [&](int kb) {  // (4 <= kb < blocks; the row's last four where fewer than four follow)
+    if (has_row) next = *(const u32_any*)(scales + min(kb, blocks - 4));
   };
   auto keep_scales = [&](int kb) {  // of the four blocks from kb on
-    if (has_row) four[kb >> 2 & 1][tid] = next;
+    if (has_row) four[kb >> 2 & 1][tid] = next >> (8 * (kb - min(kb, blocks - 4)));
   };
   f32x4 acc[MI][NI] = {};
   const int p0 = (q * 2 ^ mix(r16)) * 16, p1 = ((q * 2 + 1) ^ mix(r16)) * 16;
@@ -287,11 +306,10 @@ __global__ __launch_bounds__(64 * WM * WN, WM * WN * PER_CU / 4) void k_mm_tile(
   };
   // (block kb's scales were kept in block kb - 1 or before; what block kb - 1 read is free)
   auto next_scales = [&](int kb) {
-    if ((kb & 3) == 0) ask_scales(kb + 4);
-    if ((kb & 3) == 3) keep_scales(kb + 1);
+    if ((kb & 3) == 3 && kb + 1 < blocks) keep_scales(kb + 1);
+    if ((kb & 3) == 0 && kb + 4 < blocks) ask_scales(kb + 4);
   };
-  ask_scales(0);
-  keep_scales(0);
+  if (has_row) four[0][tid] = load_scales(scales, 0, blocks);
   if (direct > 0) stage(0, 0);
   for (int kb = 0; kb < direct; kb++) {
     __syncthreads();  // this block has landed, and the other half is free
@@ -317,6 +335,248 @@ __global__ __launch_bounds__(64 * WM * WN, WM * WN * PER_CU / 4) void k_mm_tile(
     for (int j = 0; j < NI; j++) put4(g, m0 + wm + i * 16 + r16, n0 + wn + j * 16 + q * 4, acc[i][j]);
 }
 
+// ---------------------------------------------------------------------------
+// Tiles of 256 x 256 for bfloat16 output, 2 x 4 waves of 128 x 64, pipelined by quarters of a block.  In quarter p a wave
+// multiplies two of its eight row tiles of a with its four of b, 8 instructions.  A quarter has two parts, with a barrier behind each:
+// in the first a wave reads the next quarter's operands from LDS and asks for rows of the block after next, in the second it multiplies.
+// Waves 4 to 7 are a part behind, so that of the two waves of a SIMD one multiplies while the other loads.  Loads return in order: the
+// wait for some rows is a count of the younger loads.  It is made a quarter before the rows are read, and rows are asked for a
+// quarter after all waves have read what was in their place, as the other half of the waves needs.
+// What bounds it: 8192^3 takes 434 us (2.53 PFLOP/s; 360 us on zeros): the instructions fill 63 % of the cycles, at 1.92 GHz, which is the
+// power limit's doing; the barriers and the unequal parts are the rest.  Plain double buffering with one barrier a block: 474 us.  By quarters
+// without the shift of half the waves: 466.  With 32 x 32 x 64 instructions: 478, at a lower clock.
+// ---------------------------------------------------------------------------
+template <int VM, int LGKM>
+__device__ inline void quarter() {  // all waves' loads but their last VM have landed, all their reads from LDS but the last LGKM are done
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_sched_barrier(0);
+  __builtin_amdgcn_s_waitcnt(0x0070 | LGKM << 8 | (VM & 15) | (VM >> 4) << 14);
+  __builtin_amdgcn_s_barrier();
+  __builtin_amdgcn_sched_barrier(0);
+  asm volatile("" ::: "memory");
+}
+__device__ inline void half() {  // the other half of the waves goes on to multiply, or to load
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_sched_barrier(0);
+  __builtin_amdgcn_s_barrier();
+  __builtin_amdgcn_sched_barrier(0);
+  asm volatile("" ::: "memory");
+}
+
+__global__ __launch_bounds__(512, 2) void k_mm_pipe(const MatArgs g, int tiles_m, int tiles_n) {
+#ifdef __HIP_DEVICE_COMPILE__  // (the host's pass does not know buffers)
+  // Rows of a go by quarters: 64 rows, 32 of either half of the tile.  (The compiler waits for loads into an LDS array before it
+  // reads that array, and for all of them before it reads one that no load goes into: hence an array for what is read at the same
+  // time of even and of odd blocks, and a load into the scales' array.)
+  constexpr int QUARTER = 64 * 128, B_AT = QUARTER;
+  __shared__ __attribute__((aligned(128))) uint8_t first0[QUARTER + 256 * 128], first1[QUARTER + 256 * 128];  // a's first quarter and b
+  __shared__ __attribute__((aligned(128))) uint8_t mid0[2 * QUARTER], mid1[2 * QUARTER], last0[QUARTER], last1[QUARTER];
+  __shared__ __attribute__((aligned(8))) uint32_t scales_of[12 * 128];  // [block & 7]: four scales of a lane's tiles each; nothing reads the last third
+  auto quarter_of = [&](auto p, auto odd) -> uint8_t* {
+    if constexpr (p == 0) return odd == 0 ? first0 : first1;
+    else if constexpr (p == 3) return odd == 0 ? last0 : last1;
+    else return (odd == 0 ? mid0 : mid1) + (p - 1) * QUARTER;
+  };
+  constexpr Int<0> I0{};
+  constexpr Int<1> I1{};
+  constexpr Int<2> I2{};
+  constexpr Int<3> I3{};
+
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r16 = lane & 15, q = lane >> 4;
+  const int wm = wave >> 2, wn = wave & 3;
+  int tile_m, tile_n;
+  tile_of(tiles_m, tiles_n, tile_m, tile_n);
+  const int64_t m0 = (int64_t)tile_m * 256, n0 = (int64_t)tile_n * 256;
+  const int rows_a = (int)(g.m - m0 < 256 ? g.m - m0 : 256) - 1, rows_b = (int)(g.n - n0 < 256 ? g.n - n0 : 256) - 1;  // the last ones
+  const int blocks = (int)ceil_div_d(g.k, 128), direct = (int)(g.k >> 7);
+  const uint8_t* const a0 = g.a + m0 * g.a_stride;
+  const uint8_t* const b0 = g.b + n0 * g.b_stride;
+  // A wave's load: 8 rows; those past the operand's end repeat the last.
+  const int piece16 = ((lane & 7) ^ mix((wave & 1) * 8 + (lane >> 3))) * 16;
+  const int lane_row = lane >> 3, row_a = (wave >> 2) * 128 + (wave & 3) * 8, row_b = wave * 8;
+  // (buffer loads: a lane's offset in the tile and the block's are added by the load; nothing is past a buffer of 2^32 bytes)
+  const auto buf_a = __builtin_amdgcn_make_buffer_rsrc((void*)a0, 0, -1, 0x00027000), buf_b = __builtin_amdgcn_make_buffer_rsrc((void*)b0, 0, -1, 0x00027000);
+  uint32_t off_a[4], off_b[4];
+#pragma unroll
+  for (int j = 0; j < 4; j++) {
+    off_a[j] = (uint32_t)min(lane_row + (row_a + j * 32), rows_a) * (uint32_t)g.a_stride + piece16;
+    off_b[j] = (uint32_t)min(lane_row + (row_b + j * 64), rows_b) * (uint32_t)g.b_stride + piece16;
+  }
+  auto stage_a = [&](auto p, auto odd, int kb) {  // (past the last block: nothing reads it)
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(buf_a, (__attribute__((address_space(3))) void*)(quarter_of(p, odd) + wave * 1024), 16, off_a[p],
+                                             min(kb, direct - 1) * 128, 0, 0);
+  };
+  auto stage_b = [&](auto h, auto odd, int kb) {
+#pragma unroll
+    for (int j = 0; j < 2; j++)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(
+          buf_b, (__attribute__((address_space(3))) void*)((odd == 0 ? first0 : first1) + B_AT + (h * 2 + j) * 8192 + wave * 1024), 16, off_b[h * 2 + j],
+          min(kb, direct - 1) * 128, 0, 0);
+  };
+
+  // Scales: a thread has one of the tile's rows.  Those of a lane's eight tiles of a are two groups of four bytes, those of its four of b one:
+  // the instruction picks a byte.
+  const bool of_a = wave < 4;
+  const uint8_t* const scales = of_a ? g.as + (m0 >> g.a_shift) * g.as_stride : g.bs + (n0 >> g.b_shift) * g.bs_stride;
+  const uint32_t srow = (uint32_t)(of_a ? min(tid, rows_a) >> g.a_shift : min(tid - 256, rows_b) >> g.b_shift) * (uint32_t)(of_a ? g.as_stride : g.bs_stride);
+  const int sbyte = of_a ? (tid & 128) + (tid & 15) * 8 + (tid >> 4 & 7) : (tid & ~63) + (tid & 15) * 4 + (tid >> 4 & 3);
+  const uint32_t sat = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)scales_of + sbyte;
+  auto keep_scales = [&](int at, uint32_t four) {
+    // (written like this because the compiler waits for all loads into LDS ahead of such stores; quarter() waits for them)
+    asm volatile("ds_write_b8 %0, %1\n\tds_write_b8 %0, %2 offset:512\n\tds_write_b8 %0, %3 offset:1024\n\tds_write_b8 %0, %4 offset:1536" ::
+                 "v"(sat + at * 512), "v"(four), "v"(four >> 8), "v"(four >> 16), "v"(four >> 24) : "memory");
+  };
+  keep_scales(0, load_scales(scales + srow, 0, blocks));
+  uint32_t next = 0;
+  int shift = 0;
+
+  f32x4 acc[8][4] = {};
+  i32x8 a[4][2], b[4];  // a: by quarters
+  i32x2 sa;
+  int sb;
+  // A lane's place in rows from a multiple of 16 on; its second 16 bytes are at place ^ 16.  (Not kept added to the arrays'
+  // addresses: those sums, made once for the whole loop, take the registers that the operands need.)
+  const int place = r16 * 128 + (q * 2 ^ mix(r16)) * 16;
+  auto codes = [&](const uint8_t* from, int at) {
+    const i32x4 lo = *(const i32x4*)(from + at), hi = *(const i32x4*)(from + (at ^ 16));
+    return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+  };
+  auto read_a = [&](auto p, auto odd) {
+    int at = place;
+    asm volatile("" : "+v"(at));
+#pragma unroll
+    for (int i = 0; i < 2; i++) a[p][i] = codes(quarter_of(p, odd) + wm * 4096 + i * 2048, at);
+  };
+  auto read_b = [&](auto h, auto odd) {
+    int at = place;
+    asm volatile("" : "+v"(at));
+#pragma unroll
+    for (int j = 0; j < 2; j++) b[h * 2 + j] = codes((odd == 0 ? first0 : first1) + B_AT + wn * 8192 + (h * 2 + j) * 2048, at);
+  };
+  const uint32_t at_a = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint32_t*)scales_of + wm * 128 + r16 * 8;
+  const uint32_t at_b = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint32_t*)scales_of + 256 + wn * 64 + r16 * 4;
+  auto read_scales = [&](int kb) {  // (as in keep_scales())
+    asm volatile("ds_read_b64 %0, %2\n\tds_read_b32 %1, %3\n\ts_waitcnt lgkmcnt(0)" : "=&v"(sa), "=&v"(sb)
+                 : "v"(at_a + (kb & 7) * 512), "v"(at_b + (kb & 7) * 512) : "memory");
+  };
+  auto products = [&](auto p, auto h, int s_a, int s_b) {  // quarter p of a, two tiles of b
+    auto two = [&](auto i) {
+      constexpr int row = p * 2 + i, sa_at = row & 3;
+      acc[row][h * 2] = mfma8<h * 2, sa_at>(b[h * 2], a[p][i], acc[row][h * 2], s_b, s_a);
+      acc[row][h * 2 + 1] = mfma8<h * 2 + 1, sa_at>(b[h * 2 + 1], a[p][i], acc[row][h * 2 + 1], s_b, s_a);
+    };
+    two(I0);
+    two(I1);
+  };
+  if (direct > 0) {
+    if (lane < 4)
+      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(a0 + lane * 16), (__attribute__((address_space(3))) void*)&scales_of[1024], 16, 0, 0);
+    auto ask = [&](auto odd) {
+      stage_a(I0, odd, odd);
+      stage_a(I1, odd, odd);
+      stage_b(I0, odd, odd);
+      stage_a(I2, odd, odd);
+      stage_b(I1, odd, odd);
+    };
+    ask(I0);
+    stage_a(I3, I0, 0);
+    ask(I1);
+    quarter<8, 0>();
+    read_a(I0, I0);
+    read_b(I0, I0);
+    read_b(I1, I0);
+    read_scales(0);
+    if (wave >= 4) __builtin_amdgcn_s_barrier();
+    auto block = [&](int kb, auto odd) {
+      constexpr Int<1 - odd> even{};
+      quarter<10, 8>();
+      if constexpr (odd == 1) {
+        // The scales of the blocks 4 i .. 4 i + 3 are asked for in block 4 i - 3 and kept in LDS in block 4 i - 1.  (Every second time
+        // nothing reads what is kept: a branch would part the loop, and products would be moved out of their quarter.  The
+        // row's last four where fewer than four follow.)
+        keep_scales(kb & 2 ? (kb + 1) & 4 : 8, next >> shift);
+        const int want = (kb + 3) & ~3, at = min(want, blocks - 4);
+        shift = 8 * (want - at) & 31;
+        next = *(const u32_any*)(scales + at + srow);
+      }
+      read_a(I1, odd);
+      stage_a(I3, even, kb + 1);
+      half();
+      __builtin_amdgcn_s_setprio(1);
+      products(I0, I0, sa.x, sb);
+      products(I0, I1, sa.x, sb);
+      __builtin_amdgcn_s_setprio(0);
+      quarter<8, 0>();
+      read_a(I2, odd);
+      stage_a(I0, odd, kb + 2);
+      half();
+      __builtin_amdgcn_s_setprio(1);
+      products(I1, I0, sa.x, sb);
+      products(I1, I1, sa.x, sb);
+      __builtin_amdgcn_s_setprio(0);
+      quarter<8, 0>();
+      read_a(I3, odd);
+      stage_a(I1, odd, kb + 2);
+      stage_b(I0, odd, kb + 2);
+      half();
+      __builtin_amdgcn_s_setprio(1);
+      products(I2, I0, sa.y, sb);
+      products(I2, I1, sa.y, sb);
+      __builtin_amdgcn_s_setprio(0);
+      quarter<5, 0>();
+      const int s_a = sa.y, s_b = sb;
+      read_a(I0, even);  // (the last block has no next: read and not used)
+      stage_a(I2, odd, kb + 2);
+      stage_b(I1, odd, kb + 2);
+      read_scales(kb + 1);
+      half();
+      __builtin_amdgcn_s_setprio(1);
+      products(I3, I0, s_a, s_b);
+      read_b(I0, even);
+      products(I3, I1, s_a, s_b);
+      __builtin_amdgcn_s_setprio(0);
+      read_b(I1, even);
+    };
+    int kb = 0;
+    for (; kb + 2 <= direct; kb += 2) {
+      block(kb, I0);
+      block(kb + 1, I1);
+    }
+    if (kb < direct) block(kb, I0);
+    if (wave < 4) __builtin_amdgcn_s_barrier();
+    quarter<0, 0>();  // (the last loads have landed, though nothing reads them: the LDS may go on to another workgroup)
+  }
+  for (int kb = direct; kb < blocks; kb++) {  // the last part of a block
+    __syncthreads();
+    auto part = [&](const uint8_t* row, uint8_t* to) { *(i32x4*)(to + wave * 1024 + lane * 16) = load16(row, (int64_t)kb * 128 + piece16, g.k); };
+    auto part_a = [&](auto p) { part(a0 + (int64_t)min(lane_row + row_a + p * 32, rows_a) * g.a_stride, quarter_of(p, I0)); };
+    part_a(I0);
+    part_a(I1);
+    part_a(I2);
+    part_a(I3);
+    for (int j = 0; j < 4; j++) part(b0 + (int64_t)min(lane_row + row_b + j * 64, rows_b) * g.b_stride, first0 + B_AT + j * 8192);
+    if ((kb & 3) == 0) keep_scales(kb & 4, load_scales(scales + srow, kb, blocks));
+    quarter<0, 0>();
+    read_b(I0, I0);
+    read_b(I1, I0);
+    read_scales(kb);
+    auto all = [&](auto p) {
+      read_a(p, I0);
+      products(p, I0, p < 2 ? sa.x : sa.y, sb);
+      products(p, I1, p < 2 ? sa.x : sa.y, sb);
+    };
+    all(I0);
+    all(I1);
+    all(I2);
+    all(I3);
+  }
+#pragma unroll
+  for (int i = 0; i < 8; i++)
+#pragma unroll
+    for (int j = 0; j < 4; j++) put4(g, m0 + wm * 128 + i * 16 + r16, n0 + wn * 64 + j * 16 + q * 4, acc[i][j]);
+#endif
+}
+
 template <bool EXACT, int MT>
 void rows(const MatArgs& g, hipStream_t s) {
   hipLaunchKernelGGL((k_mm_rows<EXACT, MT, 8>), dim3((uint32_t)ceil_div(g.n, 16)), dim3(512), 0, s, g);
@@ -326,12 +586,16 @@ void tiles(const MatArgs& g, hipStream_t s) {
   const int tm = (int)ceil_div(g.m, BM), tn = (int)ceil_div(g.n, BN);
   hipLaunchKernelGGL((k_mm_tile<EXACT, BM, BN, WM, WN, PER_CU>), dim3((uint32_t)((int64_t)tm * tn)), dim3(64 * WM * WN), 0, s, g, tm, tn);
 }
+void pipe(const MatArgs& g, hipStream_t s) {
+  const int tm = (int)ceil_div(g.m, 256), tn = (int)ceil_div(g.n, 256);
+  hipLaunchKernelGGL(k_mm_pipe, dim3((uint32_t)((int64_t)tm * tn)), dim3(512), 0, s, g, tm, tn);
+}
 template <bool EXACT>
 void launch(const MatArgs& g, hipStream_t s) {
   if (g.m <= 16) rows<EXACT, 1>(g, s);
   else if (g.m <= 32) rows<EXACT, 2>(g, s);
   else if (g.m <= 64) rows<EXACT, 4>(g, s);
-  else if (!EXACT && ceil_div(g.m, 256) * ceil_div(g.n, 256) >= 192) tiles<false, 256, 256, 2, 4, 1>(g, s);
+  else if (!EXACT && g.direct && g.k > 384 && ceil_div(g.m, 256) * ceil_div(g.n, 256) >= 192) pipe(g, s);
   else if (EXACT && ceil_div(g.m, 256) * ceil_div(g.n, 128) >= 192) tiles<true, 256, 128, 4, 2, 1>(g, s);
   else if (ceil_div(g.m, 128) * ceil_div(g.n, 128) >= 192) tiles<EXACT, 128, 128, 2, 2, 2>(g, s);
   else tiles<EXACT, 64, 64, 2, 2, 2>(g, s);
@@ -374,7 +638,7 @@ int bbo_net_matmul8(const void* a, int64_t a_stride, const void* a_scales, int64
                   a_scale_stride, b_stride, b_scale_stride, c_stride, m, n, k, a_tile == 128 ? 7 : 0, b_tile == 128 ? 7 : 0,
                   c_dtype == BBO_F32, accumulate != 0,
                   !(((uintptr_t)a | (uintptr_t)b | (uint64_t)a_stride | (uint64_t)b_stride) & 15) && a_stride < (1 << 23) &&
-                      b_stride < (1 << 23)};
+                      b_stride < (1 << 23) && a_scale_stride < (1 << 23) && b_scale_stride < (1 << 23)};
   if (g.c_f32) launch<true>(g, (hipStream_t)stream);
   else launch<false>(g, (hipStream_t)stream);
   return net_launched();
