@@ -11,10 +11,11 @@ the stream.  Inputs are on the GPU; calls work on the current device's current s
 import ctypes as C
 from collections import namedtuple
 
+import numpy as np
 import torch
 
 from . import binding
-from .binding import BF16, F32, OK, BboError, _new
+from .binding import BF16, F32, OK, BboError
 
 EXPORTS = ["bbo_net_rms_norm", "bbo_net_rms_norm_grad_workspace", "bbo_net_rms_norm_grad", "bbo_net_quantize",
            "bbo_net_matmul8_workspace", "bbo_net_matmul8", "bbo_net_adamw", "bbo_net_last_error"]
@@ -63,21 +64,32 @@ def _check(rc):
         raise BboError(rc, lib().bbo_net_last_error().decode())
 
 
-def _stream(stream):
-    return (torch.cuda.current_stream() if stream is None else stream).cuda_stream
+_current = torch._C._cuda_getCurrentRawStream  # of a device; torch.cuda.current_stream() takes 2.7 us to say the same
 
 
-def _matrix(t, name, dtype=None, shape=None):
-    """A [rows, cols] tensor on the GPU whose rows are dense."""
-    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+def _stream(stream, t):
+    return _current(t.get_device()) if stream is None else stream.cuda_stream
+
+
+def _room(stream, shape, stride, dtype, device):
+    """A tensor for an output: under the stream that will use it."""
+    if stream is None:
+        return torch.empty_strided(shape, stride, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty_strided(shape, stride, dtype=dtype, device=device)
+
+
+def _matrix(t, name, like=None):
+    """A [rows, cols] tensor on the GPU whose rows are dense; of another's type, shape and device."""
+    if t.dim() != 2 or (t.stride(1) != 1 and t.shape[1] > 1):
         raise ValueError("%s must be a [rows, cols] tensor with dense rows" % name)
-    if t.dtype not in _DTYPES or (dtype is not None and t.dtype != dtype):
-        raise ValueError("%s must be %s" % (name, dtype or "float32 or bfloat16"))
-    if shape is not None and t.shape != shape:
-        raise ValueError("%s must have the shape %s" % (name, tuple(shape)))
-    if t.device.type != "cuda":
-        raise ValueError("%s must be on the GPU" % name)
-    return t
+    if like is None:
+        if t.dtype not in _DTYPES:
+            raise ValueError("%s must be float32 or bfloat16" % name)
+        if not t.is_cuda:
+            raise ValueError("%s must be on the GPU" % name)
+    elif t.dtype is not like.dtype or t.shape != like.shape or t.device != like.device:
+        raise ValueError("%s must be %s %s on %s" % (name, like.dtype, tuple(like.shape), like.device))
 
 
 def _row(t):
@@ -85,42 +97,33 @@ def _row(t):
     return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
 
 
-def _vector(t, name, n):
-    if t.dtype != torch.float32 or t.dim() != 1 or t.shape[0] != n or not t.is_contiguous() or t.device.type != "cuda":
-        raise ValueError("%s must be a dense float32 [%d] tensor on the GPU" % (name, n))
-    return t
-
-
-def _same_device(*tensors):
-    first = None
-    for t in tensors:
-        if t is None:
-            continue
-        if first is None:
-            first = t.device
-        elif t.device != first:
-            raise ValueError("all tensors must be on the same GPU")
+def _vector(t, name, n, device):
+    if t.dtype is not torch.float32 or t.dim() != 1 or t.shape[0] != n or not t.is_contiguous() or t.device != device or not t.is_cuda:
+        raise ValueError("%s must be a dense float32 [%d] tensor on the same GPU" % (name, n))
 
 
 def empty_blocks8(rows, cols, tile=1, device="cuda", stream=None):
     """Room for an 8-bit matrix: rows at multiples of 128 bytes, their scales at multiples of 4."""
     kb, sr = -(-cols // BLOCK), -(-rows // tile)
-    v = _new(stream, (rows, kb * BLOCK), dtype=torch.float8_e4m3fn, device=device)
-    s = _new(stream, (sr, -(-kb // 4) * 4), dtype=torch.float8_e8m0fnu, device=device)
-    return Blocks8(v[:, :cols], s[:, :kb], tile)
+    full, sfull = kb * BLOCK, -(-kb // 4) * 4
+    v = _room(stream, (rows, full), (full, 1), torch.float8_e4m3fn, device)
+    s = _room(stream, (sr, sfull), (sfull, 1), torch.float8_e8m0fnu, device)
+    return Blocks8(v if full == cols else v[:, :cols], s if sfull == kb else s[:, :kb], tile)
 
 
 def _check_blocks(b, name):
     v, s, tile = b
-    if tile not in (1, BLOCK):
+    if tile != 1 and tile != BLOCK:
         raise ValueError("%s: tile must be 1 or 128" % name)
-    if v.dim() != 2 or v.dtype != torch.float8_e4m3fn or (v.shape[1] > 1 and v.stride(1) != 1):
+    if v.dim() != 2 or v.dtype is not torch.float8_e4m3fn or (v.stride(1) != 1 and v.shape[1] > 1):
         raise ValueError("%s: values must be float8_e4m3fn [rows, cols] with dense rows" % name)
-    want = (-(-v.shape[0] // tile), -(-v.shape[1] // BLOCK))
-    if s.dtype != torch.float8_e8m0fnu or tuple(s.shape) != want or (s.shape[1] > 1 and s.stride(1) != 1):
+    rows, cols = v.shape
+    want = (-(-rows // tile), -(-cols // BLOCK))
+    if s.dtype is not torch.float8_e8m0fnu or s.shape != want or (s.stride(1) != 1 and want[1] > 1):
         raise ValueError("%s: scales must be float8_e8m0fnu %s with dense rows" % (name, want))
-    if v.device.type != "cuda" or s.device != v.device:
+    if not v.is_cuda or s.device != v.device:
         raise ValueError("%s must be on the GPU" % name)
+    return rows, cols
 
 
 def rms_norm(x, weight=None, residual=None, eps=1e-6, want_y=True, want_rstd=False, want_8bit=False, stream=None):
@@ -129,21 +132,29 @@ def rms_norm(x, weight=None, residual=None, eps=1e-6, want_y=True, want_rstd=Fal
     weight: float32 [width] or None.  y has x's type; y8 is y in 8 bits (tile 1), rounded once.  rstd is for the gradient."""
     _matrix(x, "x")
     rows, width = x.shape
+    dtype, device = x.dtype, x.device
+    y = h = rstd = y8 = None
+    pr = pw = ph = py = ps = 0
+    r_stride, q = 0, (0, 0, 0, 0)
     if residual is not None:
-        _matrix(residual, "residual", x.dtype, x.shape)
+        _matrix(residual, "residual", x)
+        pr, r_stride = residual.data_ptr(), _row(residual)
+        h = _room(stream, (rows, width), (width, 1), dtype, device)
+        ph = h.data_ptr()
     if weight is not None:
-        _vector(weight, "weight", width)
-    _same_device(x, weight, residual)
-    new = lambda dtype, *shape: _new(stream, shape, dtype=dtype, device=x.device)
-    y = new(x.dtype, rows, width) if want_y else None
-    h = new(x.dtype, rows, width) if residual is not None else None
-    rstd = new(torch.float32, rows) if want_rstd else None
-    y8 = empty_blocks8(rows, width, 1, x.device, stream) if want_8bit else None
-    ptr = lambda t: 0 if t is None else t.data_ptr()
-    _check(lib().bbo_net_rms_norm(
-        x.data_ptr(), _row(x), ptr(residual), 0 if residual is None else _row(residual), ptr(weight), rows, width, eps, _DTYPES[x.dtype],
-        ptr(h), width, ptr(y), width, ptr(rstd), *((y8.values.data_ptr(), _row(y8.values), y8.scales.data_ptr(), _row(y8.scales)) if y8 else (0, 0, 0, 0)),
-        _stream(stream)))
+        _vector(weight, "weight", width, device)
+        pw = weight.data_ptr()
+    if want_y:
+        y = _room(stream, (rows, width), (width, 1), dtype, device)
+        py = y.data_ptr()
+    if want_rstd:
+        rstd = _room(stream, (rows,), (1,), torch.float32, device)
+        ps = rstd.data_ptr()
+    if want_8bit:
+        y8 = empty_blocks8(rows, width, 1, device, stream)
+        q = (y8.values.data_ptr(), _row(y8.values), y8.scales.data_ptr(), _row(y8.scales))
+    _check((_net or lib()).bbo_net_rms_norm(x.data_ptr(), _row(x), pr, r_stride, pw, rows, width, eps, _DTYPES[dtype], ph, width, py, width, ps, *q,
+                                            _stream(stream, x)))
     return Norm(y, h, rstd, y8)
 
 
@@ -153,26 +164,28 @@ def rms_norm_grad(dy, h, rstd, weight=None, dsum=None, want_dweight=True, worksp
     dx is the gradient of x and of residual alike; dweight (float32) is None if not wanted."""
     _matrix(h, "h")
     rows, width = h.shape
-    _matrix(dy, "dy", h.dtype, h.shape)
-    _vector(rstd, "rstd", rows)
+    dtype, device = h.dtype, h.device
+    _matrix(dy, "dy", h)
+    _vector(rstd, "rstd", rows, device)
+    pd = pw = pg = ws = room = d_stride = 0
     if dsum is not None:
-        _matrix(dsum, "dsum", h.dtype, h.shape)
+        _matrix(dsum, "dsum", h)
+        pd, d_stride = dsum.data_ptr(), _row(dsum)
     if weight is not None:
-        _vector(weight, "weight", width)
-    _same_device(h, dy, rstd, dsum, weight)
-    dx = _new(stream, (rows, width), dtype=h.dtype, device=h.device)
-    dw, room = None, 0
+        _vector(weight, "weight", width, device)
+        pw = weight.data_ptr()
+    dx, dw = _room(stream, (rows, width), (width, 1), dtype, device), None
+    L = _net or lib()
     if want_dweight:
-        dw = _new(stream, width, dtype=torch.float32, device=h.device)
+        dw = _room(stream, (width,), (1,), torch.float32, device)
+        pg = dw.data_ptr()
         if workspace is None:
             need = _SZ(0)
-            _check(lib().bbo_net_rms_norm_grad_workspace(rows, width, C.byref(need)))
-            workspace = _new(stream, max(need.value, 256), dtype=torch.uint8, device=h.device)
-        room = workspace.numel() * workspace.element_size()
-    ptr = lambda t: 0 if t is None else t.data_ptr()
-    _check(lib().bbo_net_rms_norm_grad(
-        dy.data_ptr(), _row(dy), ptr(dsum), 0 if dsum is None else _row(dsum), h.data_ptr(), _row(h), rstd.data_ptr(), ptr(weight),
-        rows, width, _DTYPES[h.dtype], dx.data_ptr(), width, ptr(dw), ptr(workspace) if want_dweight else 0, room, _stream(stream)))
+            _check(L.bbo_net_rms_norm_grad_workspace(rows, width, C.byref(need)))
+            workspace = _room(stream, (max(need.value, 256),), (1,), torch.uint8, device)
+        ws, room = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    _check(L.bbo_net_rms_norm_grad(dy.data_ptr(), _row(dy), pd, d_stride, h.data_ptr(), _row(h), rstd.data_ptr(), pw, rows, width, _DTYPES[dtype],
+                                   dx.data_ptr(), width, pg, ws, room, _stream(stream, h)))
     return dx, dw
 
 
@@ -183,44 +196,49 @@ def quantize(x, tile=1, gate=None, want_rows=True, want_cols=False, stream=None)
     ReLU; x a gradient and gate the activation's input is ReLU's gradient)."""
     _matrix(x, "x")
     rows, cols = x.shape
+    device = x.device
+    pg = g_stride = 0
     if gate is not None:
-        _matrix(gate, "gate", x.dtype, x.shape)
-    _same_device(x, gate)
-    if tile not in (1, BLOCK):
+        _matrix(gate, "gate", x)
+        pg, g_stride = gate.data_ptr(), _row(gate)
+    if tile != 1 and tile != BLOCK:
         raise ValueError("tile must be 1 or 128")
-    q = empty_blocks8(rows, cols, tile, x.device, stream) if want_rows else None
-    qt = empty_blocks8(cols, rows, tile, x.device, stream) if want_cols else None
+    q = empty_blocks8(rows, cols, tile, device, stream) if want_rows else None
+    qt = empty_blocks8(cols, rows, tile, device, stream) if want_cols else None
     part = lambda b: (b.values.data_ptr(), _row(b.values), b.scales.data_ptr(), _row(b.scales)) if b else (0, 0, 0, 0)
-    _check(lib().bbo_net_quantize(x.data_ptr(), _row(x), 0 if gate is None else gate.data_ptr(), 0 if gate is None else _row(gate),
-                                  rows, cols, _DTYPES[x.dtype], tile, *part(q), *part(qt), _stream(stream)))
+    _check((_net or lib()).bbo_net_quantize(x.data_ptr(), _row(x), pg, g_stride, rows, cols, _DTYPES[x.dtype], tile, *part(q), *part(qt),
+                                            _stream(stream, x)))
     return q, qt
 
 
 def matmul8(a, b, dtype=torch.bfloat16, out=None, accumulate=False, workspace=None, stream=None):
     """a b^T of two Blocks8 [m, k] and [n, k] -> [m, n] in float32 or bfloat16; accumulate adds to `out`."""
-    _check_blocks(a, "a")
-    _check_blocks(b, "b")
-    (m, k), n = a.values.shape, b.values.shape[0]
-    if b.values.shape[1] != k:
+    (m, k), (n, kb) = _check_blocks(a, "a"), _check_blocks(b, "b")
+    av, bv, device = a.values, b.values, a.values.device
+    if kb != k:
         raise ValueError("a and b must have rows of the same length")
     if out is None:
         if accumulate:
             raise ValueError("accumulate needs an output to add to")
         if dtype not in _DTYPES:
             raise ValueError("the output is float32 or bfloat16")
-        out = _new(stream, (m, n), dtype=dtype, device=a.values.device)
+        out = _room(stream, (m, n), (n, 1), dtype, device)
     else:
-        _matrix(out, "out", shape=(m, n))
-    _same_device(a.values, b.values, out)
+        _matrix(out, "out")
+        if out.shape != (m, n):
+            raise ValueError("out must have the shape %s" % ((m, n),))
+    if bv.device != device or out.device != device:
+        raise ValueError("all tensors must be on the same GPU")
+    L, ws, room = _net or lib(), 0, 0
     if workspace is None:
         need = _SZ(0)
-        _check(lib().bbo_net_matmul8_workspace(m, n, k, C.byref(need)))
+        _check(L.bbo_net_matmul8_workspace(m, n, k, C.byref(need)))
         if need.value:
-            workspace = _new(stream, need.value, dtype=torch.uint8, device=out.device)
-    ws, room = (0, 0) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())
-    _check(lib().bbo_net_matmul8(a.values.data_ptr(), _row(a.values), a.scales.data_ptr(), _row(a.scales), a.tile,
-                                 b.values.data_ptr(), _row(b.values), b.scales.data_ptr(), _row(b.scales), b.tile, m, n, k,
-                                 out.data_ptr(), _row(out), _DTYPES[out.dtype], int(accumulate), ws, room, _stream(stream)))
+            workspace = _room(stream, (need.value,), (1,), torch.uint8, device)
+    if workspace is not None:
+        ws, room = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    _check(L.bbo_net_matmul8(av.data_ptr(), _row(av), a.scales.data_ptr(), _row(a.scales), a.tile, bv.data_ptr(), _row(bv), b.scales.data_ptr(),
+                             _row(b.scales), b.tile, m, n, k, out.data_ptr(), _row(out), _DTYPES[out.dtype], accumulate, ws, room, _stream(stream, av)))
     return out
 
 
@@ -244,8 +262,8 @@ class AdamW:
         self.params = list(params)
         if state not in ("f32", "8bit"):
             raise ValueError("state must be f32 or 8bit")
-        if len({p.dtype for p in self.params}) > 1:
-            raise ValueError("all parameters must have one type")
+        if len({(p.dtype, p.device) for p in self.params}) > 1:
+            raise ValueError("all parameters must have one type, on one GPU")
         self.betas, self.eps, self.eight, self.seed, self.steps = betas, eps, state == "8bit", int(seed), int(step)
         n = len(self.params)
         each = lambda v: [float(x) for x in v] if isinstance(v, (list, tuple)) else [float(v)] * n
@@ -255,6 +273,9 @@ class AdamW:
         if not len(self.lr) == len(self.weight_decay) == len(self.moments) == n or (self.copies is not None and len(self.copies) != n):
             raise ValueError("lr, weight_decay, copies and moments must have one entry per parameter")
         self._table = (Tensor * max(n, 1))()
+        raw = np.frombuffer(self._table, dtype=np.uint64).reshape(-1, C.sizeof(Tensor) // 8)[:n]
+        self._at, self._rates = raw[:, :2], raw[:, 8:9].view(np.float32)  # (p, g) and (lr, weight_decay) of the records
+        self._sizes = [p.numel() for p in self.params]
         for i, p in enumerate(self.params):
             t, k = self._table[i], p.numel()
             t.p, t.n = _flat(p, "parameter", tuple(_DTYPES)), k
@@ -282,18 +303,24 @@ class AdamW:
     def step(self, grads, grad_scale=None, stream=None):
         """One step.  grads: one dense tensor per parameter, float32 or bfloat16 (one type for all); grad_scale: float32
         [1] tensor that multiplies every gradient (clipping), or None."""
-        if len(grads) != len(self.params):
+        params, n = self.params, len(self.params)
+        if len(grads) != n:
             raise ValueError("one gradient per parameter")
-        if not self.params:
+        if not n:
             return
-        dtype = grads[0].dtype
+        dtype, device = grads[0].dtype, params[0].device
         if dtype not in _DTYPES:
             raise ValueError("gradients must be float32 or bfloat16")
-        for t, p, g in zip(self._table, self.params, grads):
-            t.p, t.g = p.data_ptr(), _flat(g, "gradient", (dtype,), t.n, p.device)
-        for t, lr, wd in zip(self._table, self.lr, self.weight_decay):
-            t.lr, t.weight_decay = lr, wd
-        _check(lib().bbo_net_adamw(self._table, len(self.params), _DTYPES[self.params[0].dtype], _DTYPES[dtype], int(self.eight),
-                                   self.betas[0], self.betas[1], self.eps, self.steps + 1, self.seed,
-                                   0 if grad_scale is None else _vector(grad_scale.view(-1), "grad_scale", 1).data_ptr(), _stream(stream)))
+        for g, size in zip(grads, self._sizes):
+            if g.dtype is not dtype or g.numel() != size or not g.is_contiguous() or g.device != device:
+                raise ValueError("gradients must be dense, of the parameters' sizes, of one type and on their GPU")
+        self._at[:, 0] = [p.data_ptr() for p in params]
+        self._at[:, 1] = [g.data_ptr() for g in grads]
+        self._rates[:, 0], self._rates[:, 1] = self.lr, self.weight_decay
+        scale = 0
+        if grad_scale is not None:
+            _vector(grad_scale.view(-1), "grad_scale", 1, device)
+            scale = grad_scale.data_ptr()
+        _check((_net or lib()).bbo_net_adamw(self._table, n, _DTYPES[params[0].dtype], _DTYPES[dtype], self.eight, self.betas[0], self.betas[1], self.eps,
+                                             self.steps + 1, self.seed, scale, _stream(stream, params[0])))
         self.steps += 1
