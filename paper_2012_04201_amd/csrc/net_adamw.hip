@@ -36,19 +36,26 @@ __host__ __device__ inline uint64_t mix64(uint64_t z) {  // SplitMix64's output 
 constexpr uint64_t GOLDEN = 0x9E3779B97F4A7C15ull;
 inline uint64_t key_fold(uint64_t h, uint64_t v) { return mix64(h + (v + 1) * GOLDEN); }
 
-// e4m3 code of |t| <= 448: the lower or the upper of the two values around it, the upper with the probability of t's distance
-// from the lower (to 16 bits).  2^-120 moves e4m3's exponent range to the low end of float32's, subnormals included, where
-// the code is the upper bits.
-__device__ inline uint32_t round_random(float t, uint32_t r16, uint32_t least) {
-  const float a = __builtin_fabsf(t);
-  uint32_t code = (as_u32(a * 0x1p-120f) + (r16 << 4)) >> 20;
-  code = a > 0.f && code < least ? least : code;
-  code = a < __builtin_inff() ? code : 127;
-  return code | (t < 0.f ? 128u : 0u);
+// e4m3 code of |t| <= 448, without its sign: the lower or the upper of the two values around it, the upper with the probability of t's
+// distance from the lower (to 16 bits).  2^-120 moves e4m3's exponent range to the low end of float32's, subnormals included, where
+// the code is the upper bits.  Infinities and NaN give 127, which is NaN.  FLOOR: what is not zero gets no code of zero.
+template <bool FLOOR>
+__device__ inline uint32_t round_random(float t, uint32_t r16) {
+  const uint32_t bits = as_u32(__builtin_fabsf(t) * 0x1p-120f);
+  uint32_t code = (bits + (r16 << 4)) >> 20;
+  if (FLOOR) code = max(code, min(bits, 1u));
+  return min(code, 127u);
 }
-__device__ inline float from_code(uint32_t byte) {
-  const float a = as_f32((byte & 127) << 20) * 0x1p120f;
-  return (byte & 127) == 127 ? __builtin_nanf("") : byte & 128 ? -a : a;
+__device__ inline void from_codes(const uint32_t (&w)[2], float (&v)[8]) {
+  typedef float f32x2 __attribute__((ext_vector_type(2)));
+#pragma unroll
+  for (int i = 0; i < 2; i++) {
+    const f32x2 a = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[i], false), b = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[i], true);
+    v[4 * i] = a[0];
+    v[4 * i + 1] = a[1];
+    v[4 * i + 2] = b[0];
+    v[4 * i + 3] = b[1];
+  }
 }
 __device__ inline void load_codes(const uint8_t* p, int here, uint32_t (&w)[2]) {
   if (here >= 8) {
@@ -77,8 +84,8 @@ __global__ __launch_bounds__(256) void k_adamw(const AdamArgs a) {
   const int here = left > 8 ? 8 : left < 0 ? 0 : (int)left;
   const float gs = a.grad_scale ? *a.grad_scale : 1.f;
   float p[8], g[8], m[8], v[8];
-  load8((const P*)t.p + i0, here, p);
-  load8((const G*)t.g + i0, here, g);
+  load8((const P*)t.p + i0, i0, here, p);
+  load8((const G*)t.g + i0, i0, here, g);
 #pragma unroll
   for (int i = 0; i < 8; i++) g[i] *= gs;
   if constexpr (EIGHT) {
@@ -89,11 +96,13 @@ __global__ __launch_bounds__(256) void k_adamw(const AdamArgs a) {
     load_codes((const uint8_t*)t.m + i0, here, wm);
     load_codes((const uint8_t*)t.v + i0, here, wv);
     const float old = fmaxf(vs * a.b2, 0x1p-100f);
+    from_codes(wm, m);
+    from_codes(wv, v);
     float mtop = 0.f, vtop = 0.f;
 #pragma unroll
     for (int i = 0; i < 8; i++) {
-      m[i] = from_code(wm[i >> 2] >> (8 * (i & 3)) & 255) * ms * a.b1 + g[i] * a.c1;
-      v[i] = from_code(wv[i >> 2] >> (8 * (i & 3)) & 255) * old + g[i] * g[i] * a.c2;
+      m[i] = m[i] * ms * a.b1 + g[i] * a.c1;
+      v[i] = v[i] * old + g[i] * g[i] * a.c2;
       mtop = fmaxf(mtop, finite_abs(m[i]));
       vtop = fmaxf(vtop, finite_abs(v[i]));
     }
@@ -109,7 +118,7 @@ __global__ __launch_bounds__(256) void k_adamw(const AdamArgs a) {
     int ve = (int)(tb >> 23) - 7 - (tm <= 1.75f * om) - (tm <= 0.875f * om);
     ve = ve < 27 ? 27 : ve;
     const float vs_new = as_f32((uint32_t)ve << 23 | ob);
-    const float mi = 1.f / ms_new, vi = 1.f / vs_new;
+    const float mi = as_f32((uint32_t)(254 - me) << 23), vi = 1.f / vs_new;
     uint32_t cm[2] = {}, cv[2] = {};
 #pragma unroll
     for (int i = 0; i < 8; i += 2) {
@@ -117,8 +126,9 @@ __global__ __launch_bounds__(256) void k_adamw(const AdamArgs a) {
 #pragma unroll
       for (int k = 0; k < 2; k++) {
         const uint32_t rr = (uint32_t)(r >> (32 * k));
-        cm[(i + k) >> 2] |= round_random(m[i + k] * mi, rr & 0xffff, 0) << (8 * ((i + k) & 3));
-        cv[(i + k) >> 2] |= round_random(v[i + k] * vi, rr >> 16, 1) << (8 * ((i + k) & 3));
+        const int at = 8 * ((i + k) & 3);
+        cm[(i + k) >> 2] |= (round_random<false>(m[i + k] * mi, rr & 0xffff) | (as_u32(m[i + k]) >> 24 & 128)) << at;
+        cv[(i + k) >> 2] |= round_random<true>(v[i + k] * vi, rr >> 16) << at;
       }
     }
     store8_bytes((uint8_t*)t.m + i0, here, cm[0], cm[1]);
@@ -128,8 +138,8 @@ __global__ __launch_bounds__(256) void k_adamw(const AdamArgs a) {
       t.vs[b] = vs_new;
     }
   } else {
-    load8((const float*)t.m + i0, here, m);
-    load8((const float*)t.v + i0, here, v);
+    load8((const float*)t.m + i0, i0, here, m);
+    load8((const float*)t.v + i0, i0, here, v);
 #pragma unroll
     for (int i = 0; i < 8; i++) {
       m[i] = m[i] * a.b1 + g[i] * a.c1;
@@ -139,7 +149,8 @@ __global__ __launch_bounds__(256) void k_adamw(const AdamArgs a) {
     store8((float*)t.v + i0, here, v);
   }
 #pragma unroll
-  for (int i = 0; i < 8; i++) p[i] = p[i] * t.keep - t.step * (m[i] / (sqrtf(v[i]) * a.rbc2 + a.eps));
+  for (int i = 0; i < 8; i++)  // (root and reciprocal to 1 ulp each)
+    p[i] = p[i] * t.keep - t.step * (m[i] * __builtin_amdgcn_rcpf(__builtin_amdgcn_sqrtf(v[i]) * a.rbc2 + a.eps));
   store8((P*)t.p + i0, here, p);
   if (t.copy) store8(t.copy + i0, here, p);
 }

@@ -17,6 +17,8 @@ typedef int i32x8 __attribute__((ext_vector_type(8)));
 // Vectors at the alignment of one element: the memory pipe takes 16 bytes at any address.
 typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(1)));
 typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(1)));
+typedef uint32_t u32_any __attribute__((aligned(1)));
+typedef uint16_t u16_any __attribute__((aligned(1)));
 
 typedef uint16_t bf16;  // as bits
 
@@ -37,66 +39,154 @@ __device__ inline bf16 from_f32<bf16>(float x) {  // round to nearest, ties to e
   return __builtin_bit_cast(uint16_t, (__bf16)x);
 }
 
-// Eight values from p, of which the first `here` exist; zeros for the others.
-__device__ inline void load8(const float* p, int here, float (&v)[8]) {
-  if (here >= 8) {
-    const u32x4_any a = *(const u32x4_any*)p, b = *(const u32x4_any*)(p + 4);
+// Eight values from p, of which the first `here` exist; zeros for the others.  WHOLE: all or none do.  `before`: how many exist ahead of p,
+// so that the last few of a row are read with those in front of them, in one piece, and moved down.
+template <typename E>
+__device__ inline void load_few(const E* p, int here, float (&v)[8]) {
 #pragma unroll
-    for (int i = 0; i < 4; i++) v[i] = as_f32(a[i]), v[4 + i] = as_f32(b[i]);
-  } else {
+  for (int i = 0; i < 8; i++) v[i] = i < here ? to_f32(p[i]) : 0.f;
+}
+__device__ inline void load_all(const float* p, float (&v)[8]) {
+  const u32x4_any a = *(const u32x4_any*)p, b = *(const u32x4_any*)(p + 4);
 #pragma unroll
-    for (int i = 0; i < 8; i++) v[i] = i < here ? p[i] : 0.f;
+  for (int i = 0; i < 4; i++) v[i] = as_f32(a[i]), v[4 + i] = as_f32(b[i]);
+}
+__device__ inline void load_all(const bf16* p, float (&v)[8]) {
+  const u32x4_any a = *(const u32x4_any*)p;
+#pragma unroll
+  for (int i = 0; i < 4; i++) {
+    v[2 * i] = as_f32(a[i] << 16);
+    v[2 * i + 1] = as_f32(a[i] & 0xffff0000u);
   }
 }
-__device__ inline void load8(const bf16* p, int here, float (&v)[8]) {
-  if (here >= 8) {
-    const u32x4_any a = *(const u32x4_any*)p;
+template <int N>
+__device__ inline void move_down(bool yes, float (&v)[8]) {
 #pragma unroll
-    for (int i = 0; i < 4; i++) {
-      v[2 * i] = as_f32(a[i] << 16);
-      v[2 * i + 1] = as_f32(a[i] & 0xffff0000u);
+  for (int i = 0; i < 8; i++) v[i] = !yes ? v[i] : i + N < 8 ? v[i + N < 8 ? i + N : 0] : 0.f;
+}
+template <bool WHOLE = false, typename E>
+__device__ inline void load8(const E* p, int64_t before, int here, float (&v)[8]) {
+  if (WHOLE) {
+    if (here > 0) {
+      load_all(p, v);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; i++) v[i] = 0.f;
+    }
+    return;
+  }
+  const int gone = here >= 8 ? 0 : here <= 0 ? 8 : 8 - here;
+  if (gone <= before && gone < 8) {
+    load_all(p - gone, v);
+    if (gone) {
+      move_down<4>(gone & 4, v);
+      move_down<2>(gone & 2, v);
+      move_down<1>(gone & 1, v);
     }
   } else {
-#pragma unroll
-    for (int i = 0; i < 8; i++) v[i] = i < here ? to_f32(p[i]) : 0.f;
+    load_few(p, here, v);
   }
 }
+// Pieces of 4, 2 and 1 values where not all eight exist.
+template <bool WHOLE = false>
 __device__ inline void store8(float* p, int here, const float (&v)[8]) {
-  if (here >= 8) {
-    u32x4_any a, b;
+  u32x4_any a, b;
 #pragma unroll
-    for (int i = 0; i < 4; i++) a[i] = as_u32(v[i]), b[i] = as_u32(v[4 + i]);
+  for (int i = 0; i < 4; i++) a[i] = as_u32(v[i]), b[i] = as_u32(v[4 + i]);
+  if (here >= 8) {
     *(u32x4_any*)p = a;
     *(u32x4_any*)(p + 4) = b;
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; i++)
-      if (i < here) p[i] = v[i];
+  } else if (!WHOLE && here > 0) {
+    if (here & 4) *(u32x4_any*)p = a;
+    const bool four = here & 4;
+    float* r = p + (here & 4);
+    if (here & 2) {
+      u32x2_any c;
+      c[0] = four ? b[0] : a[0];
+      c[1] = four ? b[1] : a[1];
+      *(u32x2_any*)r = c;
+    }
+    if (here & 1) p[here - 1] = here == 1 ? v[0] : here == 3 ? v[2] : here == 5 ? v[4] : v[6];
   }
 }
+template <bool WHOLE = false>
 __device__ inline void store8(bf16* p, int here, const float (&v)[8]) {
+  u32x4_any a;
+#pragma unroll
+  for (int i = 0; i < 4; i++) a[i] = (uint32_t)from_f32<bf16>(v[2 * i]) | (uint32_t)from_f32<bf16>(v[2 * i + 1]) << 16;
   if (here >= 8) {
-    u32x4_any a;
-#pragma unroll
-    for (int i = 0; i < 4; i++) a[i] = (uint32_t)from_f32<bf16>(v[2 * i]) | (uint32_t)from_f32<bf16>(v[2 * i + 1]) << 16;
     *(u32x4_any*)p = a;
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; i++)
-      if (i < here) p[i] = from_f32<bf16>(v[i]);
+  } else if (!WHOLE && here > 0) {
+    if (here & 4) {
+      u32x2_any c;
+      c[0] = a[0];
+      c[1] = a[1];
+      *(u32x2_any*)p = c;
+    }
+    if (here & 2) *(u32_any*)(p + (here & 4)) = here & 4 ? a[2] : a[0];
+    if (here & 1) p[here - 1] = (bf16)(here == 1 ? a[0] : here == 3 ? a[1] : here == 5 ? a[2] : a[3]);
   }
 }
+// Eight values as they are in memory, for what waits in registers.  again(): what was made of them before is not kept for later.
+template <typename E>
+struct Raw;
+template <>
+struct Raw<float> {
+  float v[8];
+  template <bool WHOLE>
+  __device__ void load(const float* p, int64_t before, int here) {
+    load8<WHOLE>(p, before, here, v);
+  }
+  __device__ void get(float (&to)[8]) const {
+#pragma unroll
+    for (int i = 0; i < 8; i++) to[i] = v[i];
+  }
+  __device__ void again() {
+#pragma unroll
+    for (int i = 0; i < 8; i++) asm volatile("" : "+v"(v[i]));
+  }
+};
+template <>
+struct Raw<bf16> {
+  uint32_t w[4];
+  template <bool WHOLE>
+  __device__ void load(const bf16* p, int64_t before, int here) {
+    if (here >= 8) {
+      const u32x4_any a = *(const u32x4_any*)p;
+#pragma unroll
+      for (int i = 0; i < 4; i++) w[i] = a[i];
+    } else {
+      float v[8] = {};
+      if (!WHOLE) load8(p, before, here, v);
+#pragma unroll
+      for (int i = 0; i < 4; i++) w[i] = as_u32(v[2 * i]) >> 16 | as_u32(v[2 * i + 1]);
+    }
+  }
+  __device__ void get(float (&to)[8]) const {
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+      to[2 * i] = as_f32(w[i] << 16);
+      to[2 * i + 1] = as_f32(w[i] & 0xffff0000u);
+    }
+  }
+  __device__ void again() {
+#pragma unroll
+    for (int i = 0; i < 4; i++) asm volatile("" : "+v"(w[i]));
+  }
+};
 // Eight bytes, lowest first.
+template <bool WHOLE = false>
 __device__ inline void store8_bytes(uint8_t* p, int here, uint32_t lo, uint32_t hi) {
   if (here >= 8) {
     u32x2_any a;
     a[0] = lo;
     a[1] = hi;
     *(u32x2_any*)p = a;
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; i++)
-      if (i < here) p[i] = (uint8_t)((i < 4 ? lo : hi) >> (8 * (i & 3)));
+  } else if (!WHOLE && here > 0) {
+    if (here & 4) *(u32_any*)p = lo;
+    const uint32_t r = here & 4 ? hi : lo;
+    if (here & 2) *(u16_any*)(p + (here & 4)) = (uint16_t)r;
+    if (here & 1) p[here - 1] = (uint8_t)(here & 2 ? r >> 16 : r);
   }
 }
 
@@ -132,19 +222,18 @@ __device__ inline int scale_byte(float top) {
   return e < 0 ? 0 : e;  // (at most 247: top is finite)
 }
 __device__ inline float inverse_scale(int byte) { return as_f32((uint32_t)(254 - byte) << 23); }  // 2^(127 - byte)
-__device__ inline float e4m3_input(float x, float inv) {  // what the conversion is given: NaN stays, an infinity becomes NaN
-  return __builtin_fabsf(x) < __builtin_inff() ? x * inv : __builtin_nanf("");
+// Eight values ahead of their conversion: infinities become NaN (x - x is 0 or NaN), which a maximum leaves aside.
+__device__ inline void infinities_out(float (&v)[8]) {
+#pragma unroll
+  for (int i = 0; i < 8; i++) v[i] += v[i] - v[i];
 }
 __device__ inline uint32_t pack_e4m3(float a, float b, float c, float d) {
   int w = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
   return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, w, true);
 }
 __device__ inline void pack8_e4m3(const float (&v)[8], float inv, uint32_t& lo, uint32_t& hi) {
-  float t[8];
-#pragma unroll
-  for (int i = 0; i < 8; i++) t[i] = e4m3_input(v[i], inv);
-  lo = pack_e4m3(t[0], t[1], t[2], t[3]);
-  hi = pack_e4m3(t[4], t[5], t[6], t[7]);
+  lo = pack_e4m3(v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv);
+  hi = pack_e4m3(v[4] * inv, v[5] * inv, v[6] * inv, v[7] * inv);
 }
 
 inline bool float_type(int dtype) { return dtype == BBO_F32 || dtype == BBO_BF16; }

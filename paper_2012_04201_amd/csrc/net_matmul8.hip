@@ -166,8 +166,6 @@ __device__ inline void block_products(f32x4 (&acc)[MI][NI], const int (&sa)[MI],
   }
 }
 
-typedef uint32_t u32_any __attribute__((aligned(1)));
-
 // Four scales of a row from block kb < blocks on, block kb + i in bits 8 i; 0 past the row's end.
 __device__ inline uint32_t load_scales(const uint8_t* row, int kb, int blocks) {
   if (blocks >= 4) {  // (the last four, shifted, where fewer than four follow)

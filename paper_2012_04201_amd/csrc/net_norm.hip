@@ -41,7 +41,8 @@ struct NormArgs {
 };
 
 // One pass: a row is read once, kept in registers over the reduction and written once.
-template <typename E, int T, int NV>
+// WHOLE: the width is a multiple of eight.
+template <typename E, int T, int NV, bool WHOLE>
 __global__ __launch_bounds__(T == 64 ? 256 : T) void k_rms_norm(const NormArgs a) {
   using C = RowCut<T, NV>;
   __shared__ float slots[T > 64 ? T / 64 : 1];
@@ -50,17 +51,17 @@ __global__ __launch_bounds__(T == 64 ? 256 : T) void k_rms_norm(const NormArgs a
   float h[NV][8];
   const E* x = (const E*)a.x + row * a.x_stride;
 #pragma unroll
-  for (int v = 0; v < NV; v++) load8(x + C::col(v), a.width - C::col(v), h[v]);
+  for (int v = 0; v < NV; v++) load8<WHOLE>(x + C::col(v), C::col(v), a.width - C::col(v), h[v]);
   if (a.residual) {
     const E* r = (const E*)a.residual + row * a.residual_stride;
     E* s = (E*)a.sum + row * a.sum_stride;
 #pragma unroll
     for (int v = 0; v < NV; v++) {
       float t[8];
-      load8(r + C::col(v), a.width - C::col(v), t);
+      load8<WHOLE>(r + C::col(v), C::col(v), a.width - C::col(v), t);
 #pragma unroll
       for (int i = 0; i < 8; i++) h[v][i] = to_f32(from_f32<E>(h[v][i] + t[i]));  // as it is kept
-      store8(s + C::col(v), a.width - C::col(v), h[v]);
+      store8<WHOLE>(s + C::col(v), a.width - C::col(v), h[v]);
     }
   }
   float ss = 0.f;
@@ -76,22 +77,23 @@ __global__ __launch_bounds__(T == 64 ? 256 : T) void k_rms_norm(const NormArgs a
     const int c = C::col(v), here = a.width - c;
     if (a.weight) {
       float w[8];
-      load8(a.weight + c, here, w);
+      load8<WHOLE>(a.weight + c, c, here, w);
 #pragma unroll
       for (int i = 0; i < 8; i++) h[v][i] = h[v][i] * rstd * w[i];
     } else {
 #pragma unroll
       for (int i = 0; i < 8; i++) h[v][i] *= rstd;
     }
-    if (a.y) store8((E*)a.y + row * a.y_stride + c, here, h[v]);
+    if (a.y) store8<WHOLE>((E*)a.y + row * a.y_stride + c, here, h[v]);
     if (a.q) {
+      infinities_out(h[v]);
       float top = 0.f;
 #pragma unroll
-      for (int i = 0; i < 8; i++) top = fmaxf(top, finite_abs(h[v][i]));
+      for (int i = 0; i < 8; i++) top = fmaxf(top, __builtin_fabsf(h[v][i]));
       const int byte = scale_byte(max16(top));
       uint32_t lo, hi;
       pack8_e4m3(h[v], inverse_scale(byte), lo, hi);
-      store8_bytes(a.q + row * a.q_stride + c, here, lo, hi);
+      store8_bytes<WHOLE>(a.q + row * a.q_stride + c, here, lo, hi);
       if ((C::lane() & 15) == 0 && here > 0) a.q_scales[row * a.q_scale_stride + (c >> 7)] = (uint8_t)byte;
     }
   }
@@ -101,123 +103,155 @@ struct GradArgs {
   const void *dy, *dsum, *h;
   const float *rstd, *weight;
   void* dx;
-  float* parts;  // [groups][width], or null
+  float* parts;  // [workgroups][width], or null
   int64_t dy_stride, dsum_stride, h_stride, dx_stride, rows;
   int width, groups;
 };
 
-// Each group of T threads takes every groups-th row and keeps its share of dweight in registers; k_dweight adds the groups'.
-template <typename E, int T, int NV>
+// Each group of T threads takes every groups-th row and keeps its share of dweight in registers.  A workgroup's shares are added, and
+// k_dweight adds the workgroups'.  A row waits in registers as it is in memory (its dsum too: asked for ahead of the reduction, not behind it).
+template <typename E, int T, int NV, bool WHOLE>
 __global__ __launch_bounds__(T == 64 ? 256 : T) void k_rms_norm_grad(const GradArgs a) {
   using C = RowCut<T, NV>;
   __shared__ float slots[2][T > 64 ? T / 64 : 1];
   const int64_t group = C::group();
-  if (T == 64 && group >= a.groups) return;
-  float dw[NV][8] = {};
+  float dw[NV][8] = {}, w[NV][8];
+#pragma unroll
+  for (int v = 0; v < NV; v++) {
+    if (a.weight) {
+      load8<WHOLE>(a.weight + C::col(v), C::col(v), a.width - C::col(v), w[v]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; i++) w[v][i] = 1.f;
+    }
+  }
   int at = 0;
-  for (int64_t row = group; row < a.rows; row += a.groups, at ^= 1) {
+  // (of the last workgroup's waves some may have no group)
+  for (int64_t row = group < a.groups ? group : a.rows; row < a.rows; row += a.groups, at ^= 1) {
     const float rstd = a.rstd[row];
     const E* pg = (const E*)a.dy + row * a.dy_stride;
     const E* ph = (const E*)a.h + row * a.h_stride;
-    float g[NV][8], xh[NV][8];
+    Raw<E> g[NV], h[NV], d[NV];
 #pragma unroll
     for (int v = 0; v < NV; v++) {
       const int c = C::col(v), here = a.width - c;
-      load8(pg + c, here, g[v]);
-      load8(ph + c, here, xh[v]);
+      g[v].template load<WHOLE>(pg + c, c, here);
+      h[v].template load<WHOLE>(ph + c, c, here);
+    }
+    if (a.dsum) {
+      const E* ps = (const E*)a.dsum + row * a.dsum_stride;
+#pragma unroll
+      for (int v = 0; v < NV; v++) d[v].template load<WHOLE>(ps + C::col(v), C::col(v), a.width - C::col(v));
+    } else {
+#pragma unroll
+      for (int v = 0; v < NV; v++) d[v] = Raw<E>{};
     }
     float dot = 0.f;
 #pragma unroll
     for (int v = 0; v < NV; v++) {
-      float w[8];
-      if (a.weight) {
-        load8(a.weight + C::col(v), a.width - C::col(v), w);
-      } else {
-#pragma unroll
-        for (int i = 0; i < 8; i++) w[i] = 1.f;
-      }
+      float gv[8], xh[8];
+      g[v].get(gv);
+      h[v].get(xh);
 #pragma unroll
       for (int i = 0; i < 8; i++) {
-        xh[v][i] *= rstd;
-        dw[v][i] += g[v][i] * xh[v][i];
-        g[v][i] *= w[i];
-        dot += g[v][i] * xh[v][i];
+        xh[i] *= rstd;
+        dw[v][i] += gv[i] * xh[i];
+        dot += gv[i] * w[v][i] * xh[i];
       }
     }
     // (two sets of slots: a wave may reach the next row's sum while another still reads this row's)
     const float mean = row_sum<T>(dot, slots[at]) / (float)a.width;
-    const E* ps = a.dsum ? (const E*)a.dsum + row * a.dsum_stride : nullptr;
     E* px = (E*)a.dx + row * a.dx_stride;
 #pragma unroll
     for (int v = 0; v < NV; v++) {
-      const int c = C::col(v), here = a.width - c;
-      float d[8];
-      if (ps) {
-        load8(ps + c, here, d);
-      } else {
+      const int c = C::col(v);
+      float gv[8], xh[8], o[8];
+      g[v].again();
+      h[v].again();
+      g[v].get(gv);
+      h[v].get(xh);
+      d[v].get(o);
 #pragma unroll
-        for (int i = 0; i < 8; i++) d[i] = 0.f;
-      }
-#pragma unroll
-      for (int i = 0; i < 8; i++) d[i] += rstd * (g[v][i] - xh[v][i] * mean);
-      store8(px + c, here, d);
+      for (int i = 0; i < 8; i++) o[i] += rstd * (gv[i] * w[v][i] - xh[i] * rstd * mean);
+      store8<WHOLE>(px + c, a.width - c, o);
     }
   }
-  if (a.parts) {
+  if (!a.parts) return;
+  if constexpr (T == 64) {  // four waves' shares
+    __shared__ float share[4][64 * NV * 8];
 #pragma unroll
-    for (int v = 0; v < NV; v++) store8(a.parts + group * a.width + C::col(v), a.width - C::col(v), dw[v]);
+    for (int v = 0; v < NV; v++)
+#pragma unroll
+      for (int i = 0; i < 8; i++) share[threadIdx.x >> 6][C::col(v) + i] = dw[v][i];
+    __syncthreads();
+    for (int c = threadIdx.x; c < a.width; c += 256)
+      a.parts[(int64_t)blockIdx.x * a.width + c] = (share[0][c] + share[1][c]) + (share[2][c] + share[3][c]);
+  } else {
+#pragma unroll
+    for (int v = 0; v < NV; v++) store8<WHOLE>(a.parts + (int64_t)blockIdx.x * a.width + C::col(v), a.width - C::col(v), dw[v]);
   }
 }
 
-// dweight[c] = sum of the groups' shares, in a fixed order: 64 columns a workgroup, 16 waves that take every 16th group.
-__global__ __launch_bounds__(1024) void k_dweight(const float* parts, int groups, int width, float* dweight) {
-  __shared__ float part[16][64];
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, c = blockIdx.x * 64 + lane;
+// dweight[c] = sum of the workgroups' shares, in a fixed order: 16 columns a workgroup, every 64th share a thread.
+__global__ __launch_bounds__(1024) void k_dweight(const float* parts, int shares, int width, float* dweight) {
+  __shared__ float part[64][17];
+  const int col = threadIdx.x & 15, w = threadIdx.x >> 4, c = blockIdx.x * 16 + col;
   float s = 0.f;
   if (c < width) {
 #pragma unroll 8
-    for (int g = w; g < groups; g += 16) s += parts[(int64_t)g * width + c];
+    for (int g = w; g < shares; g += 64) s += parts[(int64_t)g * width + c];
   }
-  part[w][lane] = s;
+  part[w][col] = s;
   __syncthreads();
-  if (w == 0 && c < width) {
+  if (threadIdx.x < 16 && c < width) {
     s = 0.f;
 #pragma unroll
-    for (int i = 0; i < 16; i++) s += part[i][lane];
+    for (int i = 0; i < 64; i++) s += part[i][col];
     dweight[c] = s;
   }
 }
 
 // The cut by the width: as few threads as hold the row in registers.
-template <typename E, template <typename, int, int> class F, typename A>
-void by_width(int width, const A& a, hipStream_t s) {
-  if (width <= 512) F<E, 64, 1>::go(a, s);
-  else if (width <= 1024) F<E, 64, 2>::go(a, s);
-  else if (width <= 2048) F<E, 256, 1>::go(a, s);
-  else if (width <= 4096) F<E, 256, 2>::go(a, s);
-  else if (width <= 8192) F<E, 256, 4>::go(a, s);
-  else if (width <= 16384) F<E, 1024, 2>::go(a, s);
-  else F<E, 1024, 4>::go(a, s);
+template <typename E, template <typename, int, int, bool> class F, bool WHOLE, typename A>
+void cut(int width, const A& a, hipStream_t s) {
+  if (width <= 512) F<E, 64, 1, WHOLE>::go(a, s);
+  else if (width <= 1024) F<E, 64, 2, WHOLE>::go(a, s);
+  else if (width <= 2048) F<E, 256, 1, WHOLE>::go(a, s);
+  else if (width <= 4096) F<E, 256, 2, WHOLE>::go(a, s);
+  else if (width <= 8192) F<E, 256, 4, WHOLE>::go(a, s);
+  else if (width <= 16384) F<E, 512, 4, WHOLE>::go(a, s);
+  else F<E, 1024, 4, WHOLE>::go(a, s);
 }
-template <typename E, int T, int NV>
+template <typename E, template <typename, int, int, bool> class F, typename A>
+void by_width(int width, const A& a, hipStream_t s) {
+  if (width % 8 == 0) cut<E, F, true>(width, a, s);
+  else cut<E, F, false>(width, a, s);
+}
+template <typename E, int T, int NV, bool WHOLE>
 struct Norm {
   static void go(const NormArgs& a, hipStream_t s) {
     using C = RowCut<T, NV>;
-    hipLaunchKernelGGL((k_rms_norm<E, T, NV>), dim3((uint32_t)ceil_div(a.rows, C::PER_WG)), dim3(C::THREADS), 0, s, a);
+    hipLaunchKernelGGL((k_rms_norm<E, T, NV, WHOLE>), dim3((uint32_t)ceil_div(a.rows, C::PER_WG)), dim3(C::THREADS), 0, s, a);
   }
 };
-template <typename E, int T, int NV>
+template <typename E, int T, int NV, bool WHOLE>
 struct Grad {
   static void go(const GradArgs& a, hipStream_t s) {
     using C = RowCut<T, NV>;
-    hipLaunchKernelGGL((k_rms_norm_grad<E, T, NV>), dim3((uint32_t)ceil_div(a.groups, C::PER_WG)), dim3(C::THREADS), 0, s, a);
+    hipLaunchKernelGGL((k_rms_norm_grad<E, T, NV, WHOLE>), dim3((uint32_t)ceil_div(a.groups, C::PER_WG)), dim3(C::THREADS), 0, s, a);
   }
 };
 
-// Groups of threads that share the rows of a gradient: 2048 waves' worth, at most one per row.
+// Groups of threads that share the rows of a gradient: a wave each up to 1024 columns, a workgroup beyond; up to four to eight workgroups of
+// 256 threads a CU; with four rows each at least where that leaves two to four workgroups a CU (a share of dweight costs as much as half a row).
 int grad_groups(int64_t rows, int64_t width) {
-  const int most = width <= 1024 ? 2048 : width <= 8192 ? 1024 : 256;
-  return (int)(rows < most ? rows : most);
+  const int most = width <= 1024 ? 4096 : width <= 2048 ? 2048 : width <= 8192 ? 1024 : 512;
+  const int64_t few = width <= 2048 ? 1024 : 512, by_four = rows / 4 > few ? rows / 4 : rows < few ? rows : few;
+  return (int)(by_four < most ? by_four : most);
+}
+int grad_shares(int64_t rows, int64_t width) {
+  const int groups = grad_groups(rows, width);
+  return width <= 1024 ? (groups + 3) / 4 : groups;
 }
 
 int check_rows(int64_t rows, int64_t width, int32_t dtype) {
@@ -258,7 +292,7 @@ int bbo_net_rms_norm_grad_workspace(int64_t rows, int64_t width, size_t* out) {
   net_begin();
   if (!out) return net_fail(BBO_INVALID_ARG, "out is null");
   if (int rc = check_rows(rows, width, BBO_F32)) return rc;
-  *out = (size_t)grad_groups(rows, width) * (size_t)width * sizeof(float);
+  *out = (size_t)grad_shares(rows, width) * (size_t)width * sizeof(float);
   return BBO_OK;
 }
 
@@ -267,7 +301,7 @@ int bbo_net_rms_norm_grad(const void* dy, int64_t dy_stride, const void* dsum, i
                           void* dx, int64_t dx_stride, float* dweight, void* workspace, size_t workspace_bytes, void* stream) {
   net_begin();
   if (int rc = check_rows(rows, width, dtype)) return rc;
-  const int groups = grad_groups(rows, width);
+  const int groups = grad_groups(rows, width), shares = grad_shares(rows, width);
   hipStream_t s = (hipStream_t)stream;
   if (rows > 0) {
     if (!dy || !h || !rstd || !dx) return net_fail(BBO_INVALID_ARG, "dy/h/rstd/dx is null");
@@ -275,7 +309,7 @@ int bbo_net_rms_norm_grad(const void* dy, int64_t dy_stride, const void* dsum, i
       return net_fail(BBO_INVALID_ARG, "a stride is less than a row");
     if (dweight && !workspace) return net_fail(BBO_INVALID_ARG, "workspace is null");
     if (dweight && ((uintptr_t)workspace & 15)) return net_fail(BBO_INVALID_ARG, "workspace must be 16-byte aligned");
-    if (dweight && workspace_bytes < (size_t)groups * (size_t)width * sizeof(float))
+    if (dweight && workspace_bytes < (size_t)shares * (size_t)width * sizeof(float))
       return net_fail(BBO_WORKSPACE_TOO_SMALL, "workspace too small");
     const GradArgs a{dy, dsum, h, rstd, weight, dx, dweight ? (float*)workspace : nullptr, dy_stride, dsum_stride, h_stride,
                      dx_stride, rows, (int)width, groups};
@@ -284,7 +318,7 @@ int bbo_net_rms_norm_grad(const void* dy, int64_t dy_stride, const void* dsum, i
     if (int rc = net_launched()) return rc;
   }
   if (dweight) {
-    hipLaunchKernelGGL(k_dweight, dim3((uint32_t)ceil_div(width, 64)), dim3(1024), 0, s, (const float*)workspace, groups,
+    hipLaunchKernelGGL(k_dweight, dim3((uint32_t)ceil_div(width, 16)), dim3(1024), 0, s, (const float*)workspace, shares,
                        (int)width, dweight);
     return net_launched();
   }

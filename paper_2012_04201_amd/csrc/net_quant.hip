@@ -9,15 +9,16 @@ struct QuantArgs {
   int64_t x_stride, gate_stride, q_stride, s_stride, qt_stride, st_stride, rows, cols;
 };
 
-template <typename E>
+template <bool WHOLE = false, typename E = float>
 __device__ inline void load_gated(const QuantArgs& a, int64_t r, int64_t c, int here, float (&v)[8]) {
-  load8((const E*)a.x + r * a.x_stride + c, here, v);
+  load8<WHOLE>((const E*)a.x + r * a.x_stride + c, c, here, v);
   if (a.gate) {
     float g[8];
-    load8((const E*)a.gate + r * a.gate_stride + c, here, g);
+    load8<WHOLE>((const E*)a.gate + r * a.gate_stride + c, c, here, g);
 #pragma unroll
     for (int i = 0; i < 8; i++) v[i] = g[i] <= 0.f ? 0.f : v[i];
   }
+  infinities_out(v);
 }
 __device__ inline int clip8(int64_t here) { return here > 8 ? 8 : here < 0 ? 0 : (int)here; }
 
@@ -29,10 +30,10 @@ __global__ __launch_bounds__(256) void k_quant_rows(const QuantArgs a, int64_t b
   const int64_t r = b / blocks_per_row, kb = b - r * blocks_per_row, c = kb * 128 + (threadIdx.x & 15) * 8;
   const int here = clip8(a.cols - c);
   float v[8];
-  load_gated<E>(a, r, c, here, v);
+  load_gated<false, E>(a, r, c, here, v);
   float top = 0.f;
 #pragma unroll
-  for (int i = 0; i < 8; i++) top = fmaxf(top, finite_abs(v[i]));
+  for (int i = 0; i < 8; i++) top = fmaxf(top, __builtin_fabsf(v[i]));
   const int byte = scale_byte(max16(top));
   uint32_t lo, hi;
   pack8_e4m3(v, inverse_scale(byte), lo, hi);
@@ -41,27 +42,26 @@ __global__ __launch_bounds__(256) void k_quant_rows(const QuantArgs a, int64_t b
 }
 
 // A workgroup takes 128 x 128 values; a thread keeps 8 x 8 of them in registers, so that either order's bytes come out of it
-// in groups of eight.  The transpose goes through LDS, so that global memory sees 128 bytes side by side.
-template <typename E, int TILE>
-__global__ __launch_bounds__(256) void k_quant_tile(const QuantArgs a) {
-  __shared__ float top_of[4][128];
-  __shared__ __attribute__((aligned(16))) uint32_t turned[128][32];  // [column][rows / 4]
+// in groups of eight.  The transpose goes through LDS, so that global memory sees 128 bytes side by side.  INNER: a tile that is not cut off.
+template <typename E, int TILE, bool INNER>
+__device__ inline void quant_tile(const QuantArgs& a, int64_t tile_r, int64_t tile_c, float (&top_of)[4][128], uint2 (&turned)[128][16]) {
   const int l16 = threadIdx.x & 15, g = threadIdx.x >> 4, wave = threadIdx.x >> 6;
-  const int64_t r0 = (int64_t)blockIdx.y * 128, c0 = (int64_t)blockIdx.x * 128;
+  const int64_t r0 = tile_r * 128, c0 = tile_c * 128;
   const int64_t c = c0 + l16 * 8;
-  const int here = clip8(a.cols - c);
+  const int here = INNER ? 8 : clip8(a.cols - c);
   float v[8][8];
 #pragma unroll
   for (int i = 0; i < 8; i++) {
     const int64_t r = r0 + g * 8 + i;
-    load_gated<E>(a, r < a.rows ? r : 0, c, r < a.rows ? here : 0, v[i]);
+    if constexpr (INNER) load_gated<true, E>(a, r, c, 8, v[i]);
+    else load_gated<false, E>(a, r < a.rows ? r : 0, c, r < a.rows ? here : 0, v[i]);
   }
   float col_top[8] = {}, row_top[8] = {};
 #pragma unroll
   for (int i = 0; i < 8; i++)
 #pragma unroll
     for (int j = 0; j < 8; j++) {
-      const float t = finite_abs(v[i][j]);
+      const float t = __builtin_fabsf(v[i][j]);
       col_top[j] = fmaxf(col_top[j], t);
       row_top[i] = fmaxf(row_top[i], t);
     }
@@ -88,8 +88,8 @@ __global__ __launch_bounds__(256) void k_quant_tile(const QuantArgs a) {
       for (int j = 1; j < 8; j++) t = fmaxf(t, col_top[j]);
       byte128 = scale_byte(max16(t));
       if (threadIdx.x == 0) {
-        if (a.s) a.s[blockIdx.y * a.s_stride + blockIdx.x] = (uint8_t)byte128;
-        if (a.st) a.st[blockIdx.x * a.st_stride + blockIdx.y] = (uint8_t)byte128;
+        if (a.s) a.s[tile_r * a.s_stride + tile_c] = (uint8_t)byte128;
+        if (a.st) a.st[tile_c * a.st_stride + tile_r] = (uint8_t)byte128;
       }
     }
   }
@@ -100,9 +100,9 @@ __global__ __launch_bounds__(256) void k_quant_tile(const QuantArgs a) {
       const int byte = TILE == 128 ? byte128 : scale_byte(max16(row_top[i]));
       uint32_t lo, hi;
       pack8_e4m3(v[i], inverse_scale(byte), lo, hi);
-      if (r < a.rows) {
-        store8_bytes(a.q + r * a.q_stride + c, here, lo, hi);
-        if (TILE == 1 && l16 == 0) a.s[r * a.s_stride + blockIdx.x] = (uint8_t)byte;
+      if (INNER || r < a.rows) {
+        store8_bytes<INNER>(a.q + r * a.q_stride + c, here, lo, hi);
+        if (TILE == 1 && l16 == 0) a.s[r * a.s_stride + tile_c] = (uint8_t)byte;
       }
     }
   }
@@ -117,20 +117,27 @@ __global__ __launch_bounds__(256) void k_quant_tile(const QuantArgs a) {
       uint32_t lo, hi;
       pack8_e4m3(t, inverse_scale(byte), lo, hi);
       // groups of eight rows are swapped by the column's eight, so that 16 lanes' writes fall on different banks
-      uint32_t* to = &turned[k][(g ^ l16) * 2];
-      to[0] = lo;
-      to[1] = hi;
-      if (TILE == 1 && g == 0 && c0 + k < a.cols) a.st[(c0 + k) * a.st_stride + blockIdx.y] = (uint8_t)byte;
+      turned[k][g ^ l16] = make_uint2(lo, hi);
+      if (TILE == 1 && g == 0 && (INNER || c0 + k < a.cols)) a.st[(c0 + k) * a.st_stride + tile_r] = (uint8_t)byte;
     }
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < 8; i++) {
       const int k = i * 16 + g;  // 16 lanes write a column's 128 rows
-      const uint32_t* from = &turned[k][(l16 ^ (k >> 3)) * 2];
+      const uint2 from = turned[k][l16 ^ (k >> 3)];
       const int64_t r = r0 + l16 * 8;
-      if (c0 + k < a.cols) store8_bytes(a.qt + (c0 + k) * a.qt_stride + r, clip8(a.rows - r), from[0], from[1]);
+      if (INNER || c0 + k < a.cols) store8_bytes<INNER>(a.qt + (c0 + k) * a.qt_stride + r, INNER ? 8 : clip8(a.rows - r), from.x, from.y);
     }
   }
+}
+
+template <typename E, int TILE>
+__global__ __launch_bounds__(256) void k_quant_tile(const QuantArgs a) {
+  __shared__ float top_of[4][128];
+  __shared__ uint2 turned[128][16];  // [column][rows / 8]
+  const int64_t tile_r = gridDim.y - 1 - blockIdx.y, tile_c = blockIdx.x;  // (the bottom edge first: its tiles take longer)
+  if (tile_r * 128 + 128 <= a.rows && tile_c * 128 + 128 <= a.cols) quant_tile<E, TILE, true>(a, tile_r, tile_c, top_of, turned);
+  else quant_tile<E, TILE, false>(a, tile_r, tile_c, top_of, turned);
 }
 
 template <typename E>
