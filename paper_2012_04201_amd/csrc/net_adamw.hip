@@ -38,12 +38,13 @@ inline uint64_t key_fold(uint64_t h, uint64_t v) { return mix64(h + (v + 1) * GO
 
 // e4m3 code of |t| <= 448, without its sign: the lower or the upper of the two values around it, the upper with the probability of t's
 // distance from the lower (to 16 bits).  2^-120 moves e4m3's exponent range to the low end of float32's, subnormals included, where
-// the code is the upper bits.  Infinities and NaN give 127, which is NaN.  FLOOR: what is not zero gets no code of zero.
+// the code is the upper bits.  Infinities and NaN give 127, which is NaN.  FLOOR: what is not zero gets no code of zero (also where
+// the shift leaves nothing of it).
 template <bool FLOOR>
 __device__ inline uint32_t round_random(float t, uint32_t r16) {
-  const uint32_t bits = as_u32(__builtin_fabsf(t) * 0x1p-120f);
-  uint32_t code = (bits + (r16 << 4)) >> 20;
-  if (FLOOR) code = max(code, min(bits, 1u));
+  const float a = __builtin_fabsf(t);
+  uint32_t code = (as_u32(a * 0x1p-120f) + (r16 << 4)) >> 20;
+  if (FLOOR) code = max(code, min(as_u32(a), 1u));
   return min(code, 127u);
 }
 __device__ inline void from_codes(const uint32_t (&w)[2], float (&v)[8]) {

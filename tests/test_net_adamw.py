@@ -93,6 +93,21 @@ def test_8bit_moments_bit_for_bit(net, p_dtype, g_dtype, packed):
             gs = [g.clone() for g in gs]
 
 
+def test_8bit_second_moment_keeps_its_smallest(net):
+    """Squares of gradients from 2^-70 to 2^40 in one block: none but zero gets the code of zero, however small beside the largest."""
+    g = torch.Generator().manual_seed(5)
+    grad = torch.randn(1000, generator=g) * 2.0 ** torch.randint(-35, 20, (1000,), generator=g)
+    grad[::50] = 0
+    p = torch.zeros(1000).cuda()
+    opt = net.AdamW([p], lr=LR, betas=(B1, B2), eps=EPS, weight_decay=WD, state="8bit", seed=3)
+    zeros8, zeros = np.zeros(1000, np.uint8), np.zeros(8, np.float32)
+    opt.step([grad.cuda()])
+    s = opt.moments[0]
+    want = O.adam8(grad.numpy(), zeros8, zeros, zeros8, zeros, B1, B2, O.key_fold(O.key_fold(3, 1), 0))[4]
+    assert np.array_equal(s.v.view(torch.uint8).cpu().numpy(), want)
+    assert np.array_equal(want == 0, grad.numpy() == 0)
+
+
 def test_8bit_second_moment_decays_exactly(net):
     """Without a gradient the second moment keeps its codes, and its scale falls by beta2 a step."""
     p, g = torch.zeros(512).cuda(), torch.randn(512, generator=torch.Generator().manual_seed(4)).cuda()
