@@ -88,7 +88,7 @@ int bbo_net_quantize(const void* x, int64_t x_stride, const void* gate, int64_t 
                      int32_t dtype, int32_t tile, void* q, int64_t q_stride, void* scales, int64_t scale_stride, void* qt,
                      int64_t qt_stride, void* t_scales, int64_t t_scale_stride, void* stream);
 
-/* Bytes of workspace for bbo_net_matmul8 (0 for most shapes); writes *out. */
+/* Bytes of workspace for bbo_net_matmul8: 0, or less than 2^28 where c is small beside the contracted index; writes *out. */
 int bbo_net_matmul8_workspace(int64_t m, int64_t n, int64_t k, size_t* out);
 
 /*
@@ -100,7 +100,8 @@ int bbo_net_matmul8_workspace(int64_t m, int64_t n, int64_t k, size_t* out);
  * Sums are in float32 and rounded once.  float32 output has float32's accuracy; for bfloat16 output the matrix
  * units drop what a product has below 2^-13 of the largest among eight neighbours of the contracted index (about 1.4e-5 of
  * the result on normal data, which the output's own rounding hides).  k = 0 gives zeros (or leaves c as it is).
- *   workspace  16-byte aligned, bbo_net_matmul8_workspace() bytes; with less the same product takes longer
+ *   workspace  16-byte aligned, bbo_net_matmul8_workspace() bytes, or less (NULL for none): the same product in fewer parts, with its sums
+ *              in another order
  */
 int bbo_net_matmul8(const void* a, int64_t a_stride, const void* a_scales, int64_t a_scale_stride, int32_t a_tile, const void* b,
                     int64_t b_stride, const void* b_scales, int64_t b_scale_stride, int32_t b_tile, int64_t m, int64_t n,

@@ -22,6 +22,9 @@ struct MatArgs {
   int64_t m, n, k;
   int a_shift, b_shift;  // a scale's row is the row >> shift
   int c_f32, accumulate, direct;
+  int splits, per;  // the contracted index in parts of `per` blocks, a part a workgroup's; more than one: sums go to parts[split][m][n4]
+  float* parts;
+  int64_t n4;
 };
 
 typedef int i32x2 __attribute__((ext_vector_type(2)));
@@ -66,17 +69,45 @@ __device__ inline float scale_of(int byte) {  // 2^(byte - 127), NaN for 255
 // their sum.
 __device__ inline bool in_range(int byte) { return (uint32_t)(byte - 27) <= 200u; }
 
-// 16 bytes of a row from byte `at`, zeros past the row's end.
+// 16 bytes of a row from byte `at`, zeros past the row's end.  (Where they do not all belong to the row its last 16 are read and shifted.)
 __device__ inline i32x4 load16(const uint8_t* row, int64_t at, int64_t k) {
-  if (at + 16 <= k) return __builtin_bit_cast(i32x4, *(const u32x4_any*)(row + at));
-  i32x4 v = {0, 0, 0, 0};
-  for (int i = 0; at + i < k && i < 16; i++) v[i >> 2] |= (int)row[at + i] << (8 * (i & 3));
-  return v;
+  if (k < 16) {
+    i32x4 v = {0, 0, 0, 0};
+    for (int i = 0; at + i < k && i < 16; i++) v[i >> 2] |= (int)row[at + i] << (8 * (i & 3));
+    return v;
+  }
+  const int64_t from = at + 16 <= k ? at : k - 16;
+  const u32x4_any v = *(const u32x4_any*)(row + from);
+  const int bits = (int)(at - from) * 8;  // 0 .. 128 + 7 * 128
+  uint64_t lo = (uint64_t)v[1] << 32 | v[0], hi = (uint64_t)v[3] << 32 | v[2];
+  lo = bits >= 64 ? hi : lo;
+  hi = bits >= 64 ? 0 : hi;
+  const int rest = bits & 63;
+  lo = bits >= 128 ? 0 : lo >> rest | (hi << 1) << (63 - rest);
+  hi >>= rest;
+  return i32x4{(int)(uint32_t)lo, (int)(lo >> 32), (int)(uint32_t)hi, (int)(hi >> 32)};
+}
+
+// The part of the contracted index of this workgroup.
+__device__ inline MatArgs my_part(MatArgs g) {
+  if (g.splits > 1) {
+    const int64_t first = (int64_t)blockIdx.y * g.per, left = g.k - first * 128;
+    g.a += first * 128;
+    g.b += first * 128;
+    g.as += first;
+    g.bs += first;
+    g.k = left < g.per * 128ll ? left : g.per * 128ll;
+  }
+  return g;
 }
 
 // Four neighbouring values of c from column n on.
 __device__ inline void put4(const MatArgs& g, int64_t m, int64_t n, f32x4 v) {
   if (m >= g.m || n >= g.n) return;
+  if (g.splits > 1) {
+    *(f32x4*)(g.parts + ((int64_t)blockIdx.y * g.m + m) * g.n4 + n) = v;
+    return;
+  }
   const int here = g.n - n >= 4 ? 4 : (int)(g.n - n);
   if (g.c_f32) {
     float* c = (float*)g.c + m * g.c_stride + n;
@@ -109,9 +140,9 @@ __device__ inline void put4(const MatArgs& g, int64_t m, int64_t n, f32x4 v) {
 }
 
 // Products of one block of 128 for MI x NI tiles of 16 x 16, added to acc.  get_a(i), get_b(j): a lane's 32 codes of a row;
-// sa, sb: the rows' scales.
-template <bool EXACT, int MI, int NI, typename A, typename B>
-__device__ inline void block_products(f32x4 (&acc)[MI][NI], const int (&sa)[MI], const int (&sb)[NI], A get_a, B get_b) {
+// sa, sb: the rows' scales, in byte U.
+template <bool EXACT, int U, bool SPREAD, int MI, int NI, typename A, typename B>
+__device__ inline void block_products(f32x4 (&acc)[MI][NI], const uint32_t (&sa)[MI], const uint32_t (&sb)[NI], A get_a, B get_b) {
   if constexpr (!EXACT) {
     i32x8 b[NI];
 #pragma unroll
@@ -122,9 +153,9 @@ __device__ inline void block_products(f32x4 (&acc)[MI][NI], const int (&sa)[MI],
     for (int i = 0; i < MI; i++) {
       if (i + 1 < MI) a[(i + 1) & 1] = get_a(i + 1);
 #pragma unroll
-      for (int j = 0; j < NI; j++) acc[i][j] = mfma8(b[j], a[i & 1], acc[i][j], sb[j], sa[i]);
+      for (int j = 0; j < NI; j++) acc[i][j] = mfma8<U, U>(b[j], a[i & 1], acc[i][j], (int)sb[j], (int)sa[i]);
     }
-    if constexpr (MI > 1 && NI > 1) {  // the operand of the next products is on its way while these run
+    if constexpr (SPREAD) {  // the operand of the next products is on its way while these run
       __builtin_amdgcn_sched_group_barrier(0x100, MI + NI + 2 * NI + 2, 0);
 #pragma unroll
       for (int i = 0; i < MI; i++) {
@@ -133,19 +164,20 @@ __device__ inline void block_products(f32x4 (&acc)[MI][NI], const int (&sa)[MI],
       }
     }
   } else {
+    auto byte = [](uint32_t s) { return (int)(s >> (8 * U) & 255); };
     bool ok = true;
 #pragma unroll
-    for (int i = 0; i < MI; i++) ok &= in_range(sa[i]);
+    for (int i = 0; i < MI; i++) ok &= in_range(byte(sa[i]));
 #pragma unroll
-    for (int j = 0; j < NI; j++) ok &= in_range(sb[j]);
+    for (int j = 0; j < NI; j++) ok &= in_range(byte(sb[j]));
     const bool all = __all(ok);
     Wide b[NI];
 #pragma unroll
-    for (int j = 0; j < NI; j++) b[j] = widen(get_b(j), all ? scale_of(sb[j]) : 1.f);
+    for (int j = 0; j < NI; j++) b[j] = widen(get_b(j), all ? scale_of(byte(sb[j])) : 1.f);
     if (all) {
 #pragma unroll
       for (int i = 0; i < MI; i++) {
-        const Wide a = widen(get_a(i), scale_of(sa[i]));
+        const Wide a = widen(get_a(i), scale_of(byte(sa[i])));
 #pragma unroll
         for (int j = 0; j < NI; j++) acc[i][j] = mfma16(b[j], a, acc[i][j]);
       }
@@ -154,12 +186,12 @@ __device__ inline void block_products(f32x4 (&acc)[MI][NI], const int (&sa)[MI],
 #pragma unroll
       for (int i = 0; i < MI; i++) {
         const Wide a = widen(get_a(i), 1.f);
-        const float s = scale_of(sa[i]);
+        const float s = scale_of(byte(sa[i]));
 #pragma unroll
         for (int j = 0; j < NI; j++) {
           const f32x4 t = mfma16(b[j], a, f32x4{0.f, 0.f, 0.f, 0.f});
 #pragma unroll
-          for (int r = 0; r < 4; r++) acc[i][j][r] += t[r] * (s * scale_of(__shfl(sb[j], q4 + r)));
+          for (int r = 0; r < 4; r++) acc[i][j][r] += t[r] * (s * scale_of(__shfl(byte(sb[j]), q4 + r)));
         }
       }
     }
@@ -179,12 +211,13 @@ __device__ inline uint32_t load_scales(const uint8_t* row, int kb, int blocks) {
 
 // ---------------------------------------------------------------------------
 // Few rows: 16 columns of c a workgroup, whose waves share the contracted index.  Bound by the bytes of b, which go straight
-// to registers.
+// to registers, four blocks of a wave at once.
 // ---------------------------------------------------------------------------
 template <bool EXACT, int MT, int W>
-__global__ __launch_bounds__(64 * W) void k_mm_rows(const MatArgs g) {
+__global__ __launch_bounds__(64 * W) void k_mm_rows(const MatArgs whole) {
+  const MatArgs g = my_part(whole);
   __shared__ f32x4 part[W][MT][64];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r16 = lane & 15, q = lane >> 4;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r16 = lane & 15, q = lane >> 4;
   const int64_t n0 = (int64_t)blockIdx.x * 16;
   const int64_t nr = n0 + r16 < g.n ? n0 + r16 : g.n - 1;
   const uint8_t* b = g.b + nr * g.b_stride;
@@ -197,18 +230,47 @@ __global__ __launch_bounds__(64 * W) void k_mm_rows(const MatArgs g) {
     as[t] = g.as + (mr >> g.a_shift) * g.as_stride;
   }
   f32x4 acc[MT][1] = {};
-  const int64_t blocks = ceil_div_d(g.k, 128);
-  auto codes = [&](const uint8_t* row, int64_t at) {
-    const i32x4 lo = load16(row, at, g.k), hi = load16(row, at + 16, g.k);
-    return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-  };
-  for (int64_t kb = wave; kb < blocks; kb += W) {
-    const int64_t at = kb * 128 + q * 32;
-    int sa[MT];
-    const int sb[1] = {bs[kb]};
+  const int whole_blocks = (int)(g.k >> 7);
+  if ((g.k & 127) && wave == whole_blocks % W) {  // the last part of a block
+    const int64_t at = whole_blocks * 128ll + q * 32;
+    auto codes = [&](const uint8_t* row) {
+      const i32x4 lo = load16(row, at, g.k), hi = load16(row, at + 16, g.k);
+      return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+    };
+    uint32_t sa[MT];
+    const uint32_t sb[1] = {bs[whole_blocks]};
 #pragma unroll
-    for (int t = 0; t < MT; t++) sa[t] = as[t][kb];
-    block_products<EXACT, MT, 1>(acc, sa, sb, [&](int t) { return codes(a[t], at); }, [&](int) { return codes(b, at); });
+    for (int t = 0; t < MT; t++) sa[t] = as[t][whole_blocks];
+    block_products<EXACT, 0, false, MT, 1>(acc, sa, sb, [&](int t) { return codes(a[t]); }, [&](int) { return codes(b); });
+  }
+  constexpr int D = 4;
+  for (int first = wave; first < whole_blocks; first += W * D) {
+    i32x8 ca[D][MT], cb[D];
+    uint32_t sa[D][MT], sb[D][1];
+    auto codes = [&](const uint8_t* row, int64_t at) {
+      const u32x4_any lo = *(const u32x4_any*)(row + at), hi = *(const u32x4_any*)(row + at + 16);
+      return i32x8{(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
+    };
+#pragma unroll
+    for (int d = 0; d < D; d++) {  // (past the last block: the last again, which a zero takes out of the sum)
+      const int kb = min(first + d * W, whole_blocks - 1);
+      const int64_t at = kb * 128ll + q * 32;
+      cb[d] = codes(b, at);
+      sb[d][0] = bs[kb];
+#pragma unroll
+      for (int t = 0; t < MT; t++) {
+        ca[d][t] = codes(a[t], at);
+        sa[d][t] = as[t][kb];
+      }
+    }
+    __builtin_amdgcn_sched_barrier(0);  // (all of them are on their way)
+#pragma unroll
+    for (int d = 0; d < D; d++) {
+      const int keep = first + d * W < whole_blocks ? -1 : 0;
+#pragma unroll
+      for (int t = 0; t < MT; t++) ca[d][t] &= keep;
+      block_products<EXACT, 0, false, MT, 1>(acc, sa[d], sb[d], [&](int t) { return ca[d][t]; }, [&](int) { return cb[d]; });
+    }
   }
 #pragma unroll
   for (int t = 0; t < MT; t++) part[wave][t][lane] = acc[t][0];
@@ -241,12 +303,13 @@ __device__ inline void tile_of(int tiles_m, int tiles_n, int& tm, int& tn) {
 }
 
 template <bool EXACT, int BM, int BN, int WM, int WN, int PER_CU>
-__global__ __launch_bounds__(64 * WM * WN, WM * WN * PER_CU / 4) void k_mm_tile(const MatArgs g, int tiles_m, int tiles_n) {
+__global__ __launch_bounds__(64 * WM * WN, WM * WN * PER_CU / 4) void k_mm_tile(const MatArgs whole, int tiles_m, int tiles_n) {
   constexpr int W = WM * WN, MI = BM / WM / 16, NI = BN / WN / 16;
   constexpr int LA = BM / 8 / W, LB = BN / 8 / W;  // loads of 8 rows each by a wave
   static_assert(BM + BN <= 64 * W, "a thread for each row's scales");
   __shared__ __attribute__((aligned(128))) uint8_t lds[2][(BM + BN) * 128];
   __shared__ uint32_t four[2][BM + BN];
+  const MatArgs g = my_part(whole);
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r16 = lane & 15, q = lane >> 4;
   const int wm = wave / WN * (BM / WM), wn = wave % WN * (BN / WN);
   int tile_m, tile_n;
@@ -295,12 +358,12 @@ __global__ __launch_bounds__(64 * WM * WN, WM * WN * PER_CU / 4) void k_mm_tile(
       return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
     };
     const uint8_t* s = (const uint8_t*)&four[kb >> 2 & 1][r16] + (kb & 3);
-    int sa[MI], sb[NI];
+    uint32_t sa[MI], sb[NI];
 #pragma unroll
     for (int i = 0; i < MI; i++) sa[i] = s[(wm + i * 16) * 4];
 #pragma unroll
     for (int i = 0; i < NI; i++) sb[i] = s[(BM + wn + i * 16) * 4];
-    block_products<EXACT, MI, NI>(acc, sa, sb, [&](int i) { return frag(wm + i * 16); }, [&](int j) { return frag(BM + wn + j * 16); });
+    block_products<EXACT, 0, true, MI, NI>(acc, sa, sb, [&](int i) { return frag(wm + i * 16); }, [&](int j) { return frag(BM + wn + j * 16); });
   };
   // (block kb's scales were kept in block kb - 1 or before; what block kb - 1 read is free)
   auto next_scales = [&](int kb) {
@@ -334,6 +397,164 @@ __global__ __launch_bounds__(64 * WM * WN, WM * WN * PER_CU / 4) void k_mm_tile(
 }
 
 // ---------------------------------------------------------------------------
+// Tiles of 64 x 64 by 2 x 2 waves, where there are few: bound by the way of a block to LDS, so that three are on it while one is
+// multiplied.
+// ---------------------------------------------------------------------------
+// All waves' loads but their last VM have landed, all their reads from LDS but the last LGKM are done.
+template <int VM, int LGKM>
+__device__ inline void all_here() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_sched_barrier(0);
+  __builtin_amdgcn_s_waitcnt(0x0070 | LGKM << 8 | (VM & 15) | (VM >> 4) << 14);
+  __builtin_amdgcn_s_barrier();
+  __builtin_amdgcn_sched_barrier(0);
+  asm volatile("" ::: "memory");
+}
+
+
+template <bool EXACT>
+__global__ __launch_bounds__(256, 2) void k_mm_small(const MatArgs whole, int tiles_m, int tiles_n) {
+#ifdef __HIP_DEVICE_COMPILE__  // (the host's pass does not know buffers)
+  constexpr int BM = 64, BN = 64, WM = 2, WN = 2, W = WM * WN, MI = BM / WM / 16, NI = BN / WN / 16;
+  constexpr int LA = BM / 8 / W, LB = BN / 8 / W;  // loads of 8 rows each by a wave
+  // (An array for each block on its way: the compiler waits for loads into an LDS array before it reads that array.)
+  __shared__ __attribute__((aligned(128))) uint8_t lds0[(BM + BN) * 128], lds1[(BM + BN) * 128], lds2[(BM + BN) * 128], lds3[(BM + BN) * 128];
+  auto lds = [&](auto at) -> uint8_t* { return (at & 3) == 0 ? lds0 : (at & 3) == 1 ? lds1 : (at & 3) == 2 ? lds2 : lds3; };
+  const MatArgs g = my_part(whole);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r16 = lane & 15, q = lane >> 4;
+  const int wm = wave / WN * (BM / WM), wn = wave % WN * (BN / WN);
+  int tile_m, tile_n;
+  tile_of(tiles_m, tiles_n, tile_m, tile_n);
+  const int64_t m0 = (int64_t)tile_m * BM, n0 = (int64_t)tile_n * BN;
+  const int rows_a = (int)(g.m - m0 < BM ? g.m - m0 : BM) - 1, rows_b = (int)(g.n - n0 < BN ? g.n - n0 : BN) - 1;  // the last ones
+  const int blocks = (int)ceil_div_d(g.k, 128), direct = g.direct ? (int)(g.k >> 7) : 0;
+  const uint8_t* const a0 = g.a + m0 * g.a_stride;
+  const uint8_t* const b0 = g.b + n0 * g.b_stride;
+
+  // A lane's piece of row r: rows past the operand's end repeat the last.  (Offsets in a tile have 32 bits: the host sees to it.  A wave's
+  // rows start at multiples of 8: the same f for all its loads.)
+  const int piece = ((lane & 7) ^ mix((wave & 1) * 8 + (lane >> 3))) * 16, lane_row = wave * 8 + (lane >> 3);
+  const auto buf_a = __builtin_amdgcn_make_buffer_rsrc((void*)a0, 0, -1, 0x00027000), buf_b = __builtin_amdgcn_make_buffer_rsrc((void*)b0, 0, -1, 0x00027000);
+  uint32_t from_a[LA], from_b[LB];
+#pragma unroll
+  for (int j = 0; j < LA; j++) from_a[j] = (uint32_t)min(lane_row + j * W * 8, rows_a) * (uint32_t)g.a_stride + piece;
+#pragma unroll
+  for (int j = 0; j < LB; j++) from_b[j] = (uint32_t)min(lane_row + j * W * 8, rows_b) * (uint32_t)g.b_stride + piece;
+  auto stage = [&](auto at, int kb) {  // (past the last block: nothing reads it; a wait counts the loads behind its own)
+    const int k = min(kb, direct - 1) * 128;
+#pragma unroll
+    for (int j = 0; j < LA; j++)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(buf_a, (__attribute__((address_space(3))) void*)(lds(at) + (j * W + wave) * 1024), 16, from_a[j], k, 0, 0);
+#pragma unroll
+    for (int j = 0; j < LB; j++)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(buf_b, (__attribute__((address_space(3))) void*)(lds(at) + BM * 128 + (j * W + wave) * 1024), 16, from_b[j], k, 0, 0);
+  };
+  i32x4 rest[LA + LB];  // of a block that does not go by itself
+  auto ask_rest = [&](int kb) {
+#pragma unroll
+    for (int j = 0; j < LA; j++) rest[j] = load16(a0 + (int64_t)min(lane_row + j * W * 8, rows_a) * g.a_stride, (int64_t)kb * 128 + piece, g.k);
+#pragma unroll
+    for (int j = 0; j < LB; j++) rest[LA + j] = load16(b0 + (int64_t)min(lane_row + j * W * 8, rows_b) * g.b_stride, (int64_t)kb * 128 + piece, g.k);
+  };
+  if (direct < blocks) ask_rest(direct);
+  // Scales: those of four blocks of a lane's rows, in four bytes.
+  const uint8_t* const as = g.as + (m0 >> g.a_shift) * g.as_stride;
+  const uint8_t* const bs = g.bs + (n0 >> g.b_shift) * g.bs_stride;
+  auto scales_a = [&](int i) { return as + ((min(wm + i * 16 + r16, rows_a) + (m0 & ((1 << g.a_shift) - 1))) >> g.a_shift) * g.as_stride; };
+  auto scales_b = [&](int i) { return bs + ((min(wn + i * 16 + r16, rows_b) + (n0 & ((1 << g.b_shift) - 1))) >> g.b_shift) * g.bs_stride; };
+  uint32_t sa[MI], sb[NI];
+  f32x4 acc[MI][NI] = {};
+  const int place = r16 * 128 + (q * 2 ^ mix(r16)) * 16;  // a lane's place in 16 rows; its second 16 bytes are at place ^ 16
+  auto products = [&](auto at, auto u) {
+    auto codes = [&](const uint8_t* from) {
+      const i32x4 lo = *(const i32x4*)(from + place), hi = *(const i32x4*)(from + (place ^ 16));
+      return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+    };
+    block_products<EXACT, u, false, MI, NI>(acc, sa, sb, [&](int i) { return codes(lds(at) + (wm + i * 16) * 128); },
+                                            [&](int j) { return codes(lds(at) + (BM + wn + j * 16) * 128); });
+  };
+  // (64-bit offsets: rows of scales may be as far apart as they like)
+  uint32_t next_a[MI], next_b[NI];
+  int64_t off_a[MI], off_b[NI];
+#pragma unroll
+  for (int i = 0; i < MI; i++) {
+    next_a[i] = load_scales(scales_a(i), 0, blocks);
+    off_a[i] = scales_a(i) - as;
+  }
+#pragma unroll
+  for (int i = 0; i < NI; i++) {
+    next_b[i] = load_scales(scales_b(i), 0, blocks);
+    off_b[i] = scales_b(i) - bs;
+  }
+  int shift = 0;
+  auto next_scales = [&](int kb) {  // those of four blocks are asked for four blocks ahead (the row's last four where fewer than four follow)
+#pragma unroll
+    for (int i = 0; i < MI; i++) sa[i] = next_a[i] >> shift;
+#pragma unroll
+    for (int i = 0; i < NI; i++) sb[i] = next_b[i] >> shift;
+    if (kb + 4 < blocks) {
+      const int at = min(kb + 4, blocks - 4);
+      shift = 8 * (kb + 4 - at);
+#pragma unroll
+      for (int i = 0; i < MI; i++) next_a[i] = *(const u32_any*)(as + at + off_a[i]);
+#pragma unroll
+      for (int i = 0; i < NI; i++) next_b[i] = *(const u32_any*)(bs + at + off_b[i]);
+    }
+  };
+  if (direct > 0) {
+    stage(Int<0>{}, 0);
+    stage(Int<1>{}, 1);
+    stage(Int<2>{}, 2);
+    auto block = [&](int kb, auto u) {
+      all_here<2 * (LA + LB), 0>();  // this block has landed, and what the last one read is free
+      if constexpr (u == 0) next_scales(kb);
+      stage(Int<u + 3>{}, kb + 3);
+      products(u, u);
+    };
+    int kb = 0;
+#pragma unroll 1
+    for (; kb + 4 <= direct; kb += 4) {  // (no branches: a wait for scales would not know how many loads are behind them)
+      block(kb, Int<0>{});
+      block(kb + 1, Int<1>{});
+      block(kb + 2, Int<2>{});
+      block(kb + 3, Int<3>{});
+    }
+    if (kb < direct) block(kb++, Int<0>{});
+    if (kb < direct) block(kb++, Int<1>{});
+    if (kb < direct) block(kb++, Int<2>{});
+    if (direct & 3) {
+#pragma unroll
+      for (int i = 0; i < MI; i++) sa[i] >>= 8 * (direct & 3);
+#pragma unroll
+      for (int i = 0; i < NI; i++) sb[i] >>= 8 * (direct & 3);
+    }
+  }
+  all_here<0, 0>();  // (the last loads have landed, though nothing reads them)
+#pragma unroll 1
+  for (int kb = direct; kb < blocks; kb++) {
+    if ((kb & 3) == 0) {
+      next_scales(kb);
+    } else if (kb > direct) {
+#pragma unroll
+      for (int i = 0; i < MI; i++) sa[i] >>= 8;
+#pragma unroll
+      for (int i = 0; i < NI; i++) sb[i] >>= 8;
+    }
+#pragma unroll
+    for (int j = 0; j < LA + LB; j++) *(i32x4*)&lds0[(j * W + wave) * 1024 + lane * 16] = rest[j];
+    __syncthreads();
+    if (kb + 1 < blocks) ask_rest(kb + 1);
+    products(Int<0>{}, Int<0>{});
+    __syncthreads();
+  }
+#pragma unroll
+  for (int i = 0; i < MI; i++)
+#pragma unroll
+    for (int j = 0; j < NI; j++) put4(g, m0 + wm + i * 16 + r16, n0 + wn + j * 16 + q * 4, acc[i][j]);
+#endif
+}
+
+// ---------------------------------------------------------------------------
 // Tiles of 256 x 256 for bfloat16 output, 2 x 4 waves of 128 x 64, pipelined by quarters of a block.  In quarter p a wave
 // multiplies two of its eight row tiles of a with its four of b, 8 instructions.  A quarter has two parts, with a barrier behind each:
 // in the first a wave reads the next quarter's operands from LDS and asks for rows of the block after next, in the second it multiplies.
@@ -344,15 +565,6 @@ __global__ __launch_bounds__(64 * WM * WN, WM * WN * PER_CU / 4) void k_mm_tile(
 // power limit's doing; the barriers and the unequal parts are the rest.  Plain double buffering with one barrier a block: 474 us.  By quarters
 // without the shift of half the waves: 466.  With 32 x 32 x 64 instructions: 478, at a lower clock.
 // ---------------------------------------------------------------------------
-template <int VM, int LGKM>
-__device__ inline void quarter() {  // all waves' loads but their last VM have landed, all their reads from LDS but the last LGKM are done
-  asm volatile("" ::: "memory");
-  __builtin_amdgcn_sched_barrier(0);
-  __builtin_amdgcn_s_waitcnt(0x0070 | LGKM << 8 | (VM & 15) | (VM >> 4) << 14);
-  __builtin_amdgcn_s_barrier();
-  __builtin_amdgcn_sched_barrier(0);
-  asm volatile("" ::: "memory");
-}
 __device__ inline void half() {  // the other half of the waves goes on to multiply, or to load
   asm volatile("" ::: "memory");
   __builtin_amdgcn_sched_barrier(0);
@@ -420,7 +632,7 @@ __global__ __launch_bounds__(512, 2) void k_mm_pipe(const MatArgs g, int tiles_m
   const int sbyte = of_a ? (tid & 128) + (tid & 15) * 8 + (tid >> 4 & 7) : (tid & ~63) + (tid & 15) * 4 + (tid >> 4 & 3);
   const uint32_t sat = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)scales_of + sbyte;
   auto keep_scales = [&](int at, uint32_t four) {
-    // (written like this because the compiler waits for all loads into LDS ahead of such stores; quarter() waits for them)
+    // (written like this because the compiler waits for all loads into LDS ahead of such stores; all_here() waits for them)
     asm volatile("ds_write_b8 %0, %1\n\tds_write_b8 %0, %2 offset:512\n\tds_write_b8 %0, %3 offset:1024\n\tds_write_b8 %0, %4 offset:1536" ::
                  "v"(sat + at * 512), "v"(four), "v"(four >> 8), "v"(four >> 16), "v"(four >> 24) : "memory");
   };
@@ -479,7 +691,7 @@ __global__ __launch_bounds__(512, 2) void k_mm_pipe(const MatArgs g, int tiles_m
     ask(I0);
     stage_a(I3, I0, 0);
     ask(I1);
-    quarter<8, 0>();
+    all_here<8, 0>();
     read_a(I0, I0);
     read_b(I0, I0);
     read_b(I1, I0);
@@ -487,7 +699,7 @@ __global__ __launch_bounds__(512, 2) void k_mm_pipe(const MatArgs g, int tiles_m
     if (wave >= 4) __builtin_amdgcn_s_barrier();
     auto block = [&](int kb, auto odd) {
       constexpr Int<1 - odd> even{};
-      quarter<10, 8>();
+      all_here<10, 8>();
       if constexpr (odd == 1) {
         // The scales of the blocks 4 i .. 4 i + 3 are asked for in block 4 i - 3 and kept in LDS in block 4 i - 1.  (Every second time
         // nothing reads what is kept: a branch would part the loop, and products would be moved out of their quarter.  The
@@ -504,7 +716,7 @@ __global__ __launch_bounds__(512, 2) void k_mm_pipe(const MatArgs g, int tiles_m
       products(I0, I0, sa.x, sb);
       products(I0, I1, sa.x, sb);
       __builtin_amdgcn_s_setprio(0);
-      quarter<8, 0>();
+      all_here<8, 0>();
       read_a(I2, odd);
       stage_a(I0, odd, kb + 2);
       half();
@@ -512,7 +724,7 @@ __global__ __launch_bounds__(512, 2) void k_mm_pipe(const MatArgs g, int tiles_m
       products(I1, I0, sa.x, sb);
       products(I1, I1, sa.x, sb);
       __builtin_amdgcn_s_setprio(0);
-      quarter<8, 0>();
+      all_here<8, 0>();
       read_a(I3, odd);
       stage_a(I1, odd, kb + 2);
       stage_b(I0, odd, kb + 2);
@@ -521,7 +733,7 @@ __global__ __launch_bounds__(512, 2) void k_mm_pipe(const MatArgs g, int tiles_m
       products(I2, I0, sa.y, sb);
       products(I2, I1, sa.y, sb);
       __builtin_amdgcn_s_setprio(0);
-      quarter<5, 0>();
+      all_here<5, 0>();
       const int s_a = sa.y, s_b = sb;
       read_a(I0, even);  // (the last block has no next: read and not used)
       stage_a(I2, odd, kb + 2);
@@ -542,7 +754,7 @@ __global__ __launch_bounds__(512, 2) void k_mm_pipe(const MatArgs g, int tiles_m
     }
     if (kb < direct) block(kb, I0);
     if (wave < 4) __builtin_amdgcn_s_barrier();
-    quarter<0, 0>();  // (the last loads have landed, though nothing reads them: the LDS may go on to another workgroup)
+    all_here<0, 0>();  // (the last loads have landed, though nothing reads them: the LDS may go on to another workgroup)
   }
   for (int kb = direct; kb < blocks; kb++) {  // the last part of a block
     __syncthreads();
@@ -554,7 +766,7 @@ __global__ __launch_bounds__(512, 2) void k_mm_pipe(const MatArgs g, int tiles_m
     part_a(I3);
     for (int j = 0; j < 4; j++) part(b0 + (int64_t)min(lane_row + row_b + j * 64, rows_b) * g.b_stride, first0 + B_AT + j * 8192);
     if ((kb & 3) == 0) keep_scales(kb & 4, load_scales(scales + srow, kb, blocks));
-    quarter<0, 0>();
+    all_here<0, 0>();
     read_b(I0, I0);
     read_b(I1, I0);
     read_scales(kb);
@@ -575,28 +787,98 @@ __global__ __launch_bounds__(512, 2) void k_mm_pipe(const MatArgs g, int tiles_m
 #endif
 }
 
+// c (+)= the sum of the parts, in their order: four columns a thread.  (The parts have less than 2^28 bytes.)
+__global__ __launch_bounds__(256) void k_mm_join(const MatArgs whole) {
+  MatArgs g = whole;
+  const uint32_t id = blockIdx.x * 256 + threadIdx.x, per_row = (uint32_t)g.n4 >> 2, m = id / per_row, n = (id - m * per_row) * 4;
+  if (m >= g.m) return;
+  const float* from = g.parts + (uint64_t)m * g.n4 + n;
+  f32x4 s = *(const f32x4*)from;
+  for (int i = 1; i < whole.splits; i++) s += *(const f32x4*)(from += g.m * g.n4);
+  g.splits = 1;
+  put4(g, m, n, s);
+}
+
 template <bool EXACT, int MT>
 void rows(const MatArgs& g, hipStream_t s) {
-  hipLaunchKernelGGL((k_mm_rows<EXACT, MT, 8>), dim3((uint32_t)ceil_div(g.n, 16)), dim3(512), 0, s, g);
+  hipLaunchKernelGGL((k_mm_rows<EXACT, MT, 8>), dim3((uint32_t)ceil_div(g.n, 16), g.splits), dim3(512), 0, s, g);
 }
 template <bool EXACT, int BM, int BN, int WM, int WN, int PER_CU>
 void tiles(const MatArgs& g, hipStream_t s) {
   const int tm = (int)ceil_div(g.m, BM), tn = (int)ceil_div(g.n, BN);
-  hipLaunchKernelGGL((k_mm_tile<EXACT, BM, BN, WM, WN, PER_CU>), dim3((uint32_t)((int64_t)tm * tn)), dim3(64 * WM * WN), 0, s, g, tm, tn);
+  hipLaunchKernelGGL((k_mm_tile<EXACT, BM, BN, WM, WN, PER_CU>), dim3((uint32_t)((int64_t)tm * tn), g.splits), dim3(64 * WM * WN), 0, s, g, tm, tn);
+}
+template <bool EXACT>
+void small(const MatArgs& g, hipStream_t s) {
+  const int tm = (int)ceil_div(g.m, 64), tn = (int)ceil_div(g.n, 64);
+  hipLaunchKernelGGL(k_mm_small<EXACT>, dim3((uint32_t)((int64_t)tm * tn), g.splits), dim3(256), 0, s, g, tm, tn);
 }
 void pipe(const MatArgs& g, hipStream_t s) {
   const int tm = (int)ceil_div(g.m, 256), tn = (int)ceil_div(g.n, 256);
   hipLaunchKernelGGL(k_mm_pipe, dim3((uint32_t)((int64_t)tm * tn)), dim3(512), 0, s, g, tm, tn);
 }
+
+// Which kernel, and in how many parts of the contracted index: the one that takes least by its measured time for a block of 128.  A
+// workgroup of 128 x 128 (of 64 x 64) alone on its CU takes 0.76 (0.34) us a block for bfloat16 output and 1.6 (0.6) for
+// float32, two together 1.1 (0.48) and 2.3 (0.84); 256 x 256 takes 1.75.  Parts cost the join's launch and 8 bytes of every
+// value a part at 3 TB/s.  us, one kernel against another: 4096^3 61 / 76 / 148 by falling size; 20000 x 1024 x 4096 105 / 97 / 180;
+// 2048^2 x 4096 50 / 29 / 41; 1024^2 x 4096 49 / 28 / 16.  One part against the chosen number: 1000 x 512 x 20000 59 / 33, float32 102 /
+// 43; 100 x 100 x 16000 44 / 13, float32 80 / 18; 4096 x 1024 x 20000 in float32 253 / 192.  Up to 32 rows go to
+// k_mm_rows (16 x 4096 x 4096 10.0 us, 64 x 64 tiles in four parts 11.5; 32 rows 12.7 / 12.4, in float32 12.9 / 14.7; 33 rows
+// 13.9 / 12.1), which is in parts where its workgroups are few (1 x 100 x 16000 16 / 9.5).
+enum Kernel { ROWS, SMALL, LARGE, PIPE };
+struct Plan {
+  Kernel kernel;
+  int64_t splits, per;
+};
+int64_t padded4(int64_t n) { return (n + 3) & ~3ll; }
+int64_t parts_bytes(const Plan& p, int64_t m, int64_t n) { return p.splits > 1 ? p.splits * m * padded4(n) * 4 : 0; }
+// (pipe_too: the operands' rows are as k_mm_pipe needs them; room: bytes of workspace)
+Plan plan_of(bool exact, bool pipe_too, int64_t m, int64_t n, int64_t k, size_t room) {
+  const int64_t blocks = ceil_div(k, 128);
+  Plan best{SMALL, 1, blocks};
+  double least = 1e300;
+  const double values = (double)m * padded4(n);
+  const double most = (double)(room < (1u << 28) - 1 ? room : (1u << 28) - 1) / 4 / values;  // parts that there is room for
+  auto offer = [&](Kernel kernel, int64_t s, double us) {
+    if (s > 1) us += 3 + s * values * 8 / 3e6;
+    if (us < least) least = us, best = Plan{kernel, s, ceil_div(blocks, s)};
+  };
+  if (m <= 32) {  // (eight waves share a part's blocks)
+    const int64_t groups = ceil_div(n, 16);
+    for (int64_t s = 1; s == 1 || (s <= 16 && s * 8 <= blocks && s <= most && groups * s <= 512); s++)
+      offer(ROWS, s, 0.75 * (double)ceil_div(ceil_div(blocks, s), 8));
+  } else {
+    auto rounds = [](int64_t groups, double one, double two) {
+      const int64_t last = groups & 511;
+      return (double)(groups >> 9) * two + (last == 0 ? 0 : last <= 256 ? one : two);
+    };
+    const int64_t large = ceil_div(m, 128) * ceil_div(n, 128), small = ceil_div(m, 64) * ceil_div(n, 64);
+    if (pipe_too && k > 384) offer(PIPE, 1, 1.75 * (double)(ceil_div(ceil_div(m, 256) * ceil_div(n, 256), 256) * blocks));
+    for (int64_t s = 1; s == 1 || (s <= 16 && s * 4 <= blocks && s <= most && large * s <= 1024); s++) {
+      const double each = (double)ceil_div(blocks, s);
+      offer(LARGE, s, each * rounds(large * s, exact ? 1.6 : 0.76, exact ? 2.3 : 1.1));
+      offer(SMALL, s, each * rounds(small * s, exact ? 0.6 : 0.34, exact ? 0.84 : 0.48));
+    }
+  }
+  best.splits = best.per > 0 ? ceil_div(blocks, best.per) : 1;  // (no empty part)
+  return best;
+}
+
 template <bool EXACT>
-void launch(const MatArgs& g, hipStream_t s) {
-  if (g.m <= 16) rows<EXACT, 1>(g, s);
-  else if (g.m <= 32) rows<EXACT, 2>(g, s);
-  else if (g.m <= 64) rows<EXACT, 4>(g, s);
-  else if (!EXACT && g.direct && g.k > 384 && ceil_div(g.m, 256) * ceil_div(g.n, 256) >= 192) pipe(g, s);
-  else if (EXACT && ceil_div(g.m, 256) * ceil_div(g.n, 128) >= 192) tiles<true, 256, 128, 4, 2, 1>(g, s);
-  else if (ceil_div(g.m, 128) * ceil_div(g.n, 128) >= 192) tiles<EXACT, 128, 128, 2, 2, 2>(g, s);
-  else tiles<EXACT, 64, 64, 2, 2, 2>(g, s);
+void launch(MatArgs& g, void* workspace, size_t room, hipStream_t s) {
+  const Plan p = plan_of(EXACT, !EXACT && g.direct, g.m, g.n, g.k, room);
+  g.splits = (int)p.splits;
+  g.per = (int)p.per;
+  g.parts = (float*)workspace;
+  g.n4 = padded4(g.n);
+  switch (p.kernel) {
+    case ROWS: g.m <= 16 ? rows<EXACT, 1>(g, s) : rows<EXACT, 2>(g, s); break;
+    case SMALL: small<EXACT>(g, s); break;
+    case LARGE: tiles<EXACT, 128, 128, 2, 2, 2>(g, s); break;
+    case PIPE: if constexpr (!EXACT) pipe(g, s); break;
+  }
+  if (g.splits > 1) hipLaunchKernelGGL(k_mm_join, dim3((uint32_t)ceil_div(g.m * (g.n4 >> 2), 256)), dim3(256), 0, s, g);
 }
 
 }  // namespace
@@ -607,7 +889,12 @@ int bbo_net_matmul8_workspace(int64_t m, int64_t n, int64_t k, size_t* out) {
   net_begin();
   if (!out) return net_fail(BBO_INVALID_ARG, "out is null");
   if (m < 0 || n < 0 || k < 0) return net_fail(BBO_INVALID_ARG, "m, n or k < 0");
-  *out = 0;
+  size_t most = 0;
+  for (int i = 0; i < 3; i++) {
+    const size_t bytes = (size_t)parts_bytes(plan_of(i == 0, i == 1, m, n, k, SIZE_MAX), m, n);
+    if (bytes > most) most = bytes;
+  }
+  *out = most;
   return BBO_OK;
 }
 
@@ -630,15 +917,16 @@ int bbo_net_matmul8(const void* a, int64_t a_stride, const void* a_scales, int64
     if (a_stride < k || b_stride < k || a_scale_stride < ceil_div(k, 128) || b_scale_stride < ceil_div(k, 128))
       return net_fail(BBO_INVALID_ARG, "a stride is less than a row");
   }
-  (void)workspace;
-  (void)workspace_bytes;
-  const MatArgs g{(const uint8_t*)a, (const uint8_t*)a_scales, (const uint8_t*)b, (const uint8_t*)b_scales, c, a_stride,
+  if (workspace && ((uintptr_t)workspace & 15)) return net_fail(BBO_INVALID_ARG, "workspace must be 16-byte aligned");
+  if (!workspace) workspace_bytes = 0;
+  MatArgs g{(const uint8_t*)a, (const uint8_t*)a_scales, (const uint8_t*)b, (const uint8_t*)b_scales, c, a_stride,
                   a_scale_stride, b_stride, b_scale_stride, c_stride, m, n, k, a_tile == 128 ? 7 : 0, b_tile == 128 ? 7 : 0,
                   c_dtype == BBO_F32, accumulate != 0,
                   !(((uintptr_t)a | (uintptr_t)b | (uint64_t)a_stride | (uint64_t)b_stride) & 15) && a_stride < (1 << 23) &&
-                      b_stride < (1 << 23) && a_scale_stride < (1 << 23) && b_scale_stride < (1 << 23)};
-  if (g.c_f32) launch<true>(g, (hipStream_t)stream);
-  else launch<false>(g, (hipStream_t)stream);
+                      b_stride < (1 << 23) && a_scale_stride < (1 << 23) && b_scale_stride < (1 << 23),
+                  1, 0, nullptr, 0};
+  if (g.c_f32) launch<true>(g, workspace, workspace_bytes, (hipStream_t)stream);
+  else launch<false>(g, workspace, workspace_bytes, (hipStream_t)stream);
   return net_launched();
 }
 

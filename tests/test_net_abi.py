@@ -46,8 +46,8 @@ def quant(net, x=P, xs=200, gate=0, gs=200, rows=4, cols=200, dt=0, tile=1, q=P,
     return net.lib().bbo_net_quantize(x, xs, gate, gs, rows, cols, dt, tile, q, qs, s, ss, qt, qts, st, sts, 0)
 
 
-def mm(net, a=P, a_s=256, sa=P, sas=4, at=1, b=P, b_s=256, sb=P, sbs=4, bt=1, m=4, n=8, k=200, c=P, cs=8, dt=0, acc=0):
-    return net.lib().bbo_net_matmul8(a, a_s, sa, sas, at, b, b_s, sb, sbs, bt, m, n, k, c, cs, dt, acc, 0, 0, 0)
+def mm(net, a=P, a_s=256, sa=P, sas=4, at=1, b=P, b_s=256, sb=P, sbs=4, bt=1, m=4, n=8, k=200, c=P, cs=8, dt=0, acc=0, ws=0, room=0):
+    return net.lib().bbo_net_matmul8(a, a_s, sa, sas, at, b, b_s, sb, sbs, bt, m, n, k, c, cs, dt, acc, ws, room, 0)
 
 
 def adam(net, n=10, count=1, p=P, g=P, m=P, v=P, ms=0, vs=0, copy=0, lr=1e-3, wd=0.0, pd=0, gd=0, moments=0, b1=0.9, b2=0.999, eps=1e-8, step=1, table=True):
@@ -72,7 +72,7 @@ INVALID, UNSUPPORTED, SMALL = 1, 2, 3
     (quant, dict(rows=1 << 40), UNSUPPORTED),
     (mm, dict(m=-1), INVALID), (mm, dict(at=2), INVALID), (mm, dict(bt=0), INVALID), (mm, dict(dt=9), INVALID), (mm, dict(c=0), INVALID),
     (mm, dict(cs=7), INVALID), (mm, dict(a=0), INVALID), (mm, dict(sb=0), INVALID), (mm, dict(a_s=199), INVALID),
-    (mm, dict(sbs=1), INVALID), (mm, dict(m=1 << 40), UNSUPPORTED),
+    (mm, dict(sbs=1), INVALID), (mm, dict(ws=BAD_ALIGNED, room=64), INVALID), (mm, dict(m=1 << 40), UNSUPPORTED),
     (adam, dict(count=-1), INVALID), (adam, dict(pd=3), INVALID), (adam, dict(moments=2), INVALID), (adam, dict(b1=1.0), INVALID),
     (adam, dict(b2=-0.1), INVALID), (adam, dict(eps=float("nan")), INVALID), (adam, dict(step=0), INVALID), (adam, dict(table=False), INVALID),
     (adam, dict(n=-1), INVALID), (adam, dict(p=0), INVALID), (adam, dict(v=0), INVALID), (adam, dict(moments=1), INVALID),
@@ -91,6 +91,11 @@ def test_nothing_to_do_is_no_error(net):
     out = net._SZ(7)
     assert net.lib().bbo_net_matmul8_workspace(4, 4, 4, C.byref(out)) == 0
     assert net.lib().bbo_net_matmul8_workspace(-4, 4, 4, C.byref(out)) == INVALID
+    assert net.lib().bbo_net_matmul8_workspace(100, 100, 16000, C.byref(out)) == 0 and out.value >= 2 * 100 * 100 * 4
+    for m, n, k in ((4096, 4096, 4096), (20000, 20000, 1 << 30), (1, 4096, 128), (0, 5, 5), (5, 0, 5), (5, 5, 0), (2**31 - 1, 2**31 - 1, 2**31 - 1)):
+        assert net.lib().bbo_net_matmul8_workspace(m, n, k, C.byref(out)) == 0 and out.value == 0, (m, n, k)
+    for m, n, k in ((700, 10000, 100000), (5000, 5000, 10**6), (32, 2000, 10**6), (128, 128, 10**9)):
+        assert net.lib().bbo_net_matmul8_workspace(m, n, k, C.byref(out)) == 0 and out.value < 1 << 28, (m, n, k)
     assert net.lib().bbo_net_rms_norm_grad_workspace(3, 100, C.byref(out)) == 0 and out.value >= 100 * 4
 
 

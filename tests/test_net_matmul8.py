@@ -84,6 +84,17 @@ def test_many_tiles(net, m, n, k):
     check(net.matmul8(a, b, dtype=torch.float32), a, b)
 
 
+@pytest.mark.parametrize("m,n,k", [(3300, 4000, 385), (3333, 3845, 512), (3400, 3840, 640), (3585, 3601, 900), (3300, 4000, 1024), (6200, 1900, 1151)])
+def test_many_large_tiles(net, m, n, k):
+    """Largest tiles, ragged at every edge; odd and even numbers of blocks, whole and with a part at the end."""
+    a, b = matrix(net, m, k, 1, 18), matrix(net, n, k, 128 if k & 1 else 1, 19)
+    got = net.matmul8(a, b)
+    check(got, a, b)
+    c0 = (torch.randn(m, n, generator=torch.Generator().manual_seed(3)) * 10).bfloat16().cuda()
+    check(net.matmul8(a, b, out=c0.clone(), accumulate=True), a, b, c0)
+    assert all(torch.equal(got, net.matmul8(a, b)) for _ in range(3))
+
+
 @pytest.mark.parametrize("m", [1, 40, 200])
 def test_scales_from_one_end_to_the_other(net, m):
     """Scales down to 2^-127 and up to 2^100, zeros under the largest, and NaN as value and as scale."""
@@ -143,6 +154,53 @@ def test_accuracy_on_normal_data(net):
         got = net.matmul8(a, b).cpu()
         away = (got.double() - want).abs() > (want.bfloat16().double() - want).abs() + 1e-3 * want.abs()
         assert float(away.double().mean()) < 0.02  # rounded the other way than the exact result would be
+
+
+@pytest.mark.parametrize("m,n,k", [(1, 100, 16000), (20, 33, 9001), (33, 50, 3000), (100, 100, 16000), (130, 127, 5000), (250, 130, 20001), (2100, 600, 9000)])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_the_contracted_index_in_parts(net, m, n, k, dtype):
+    """Few tiles and long rows: with the workspace that the product asks for, with some of it and with none."""
+    import ctypes as C
+    a, b = matrix(net, m, k, 1, 20), matrix(net, n, k, 128, 21)
+    need = C.c_size_t()
+    assert net.lib().bbo_net_matmul8_workspace(m, n, k, C.byref(need)) == 0 and need.value % (4 * m) == 0 and need.value > 4 * m * n
+    c0 = (torch.randn(m, n, generator=torch.Generator().manual_seed(22)) * 10).to(dtype).cuda()
+    for size in (need.value, need.value - 1, need.value // 2, 2 * m * (n + 3) * 4, 100, 0):
+        ws = torch.full((size + 64,), 255, dtype=torch.uint8).cuda()
+        got = net.matmul8(a, b, dtype=dtype, workspace=ws[:size])
+        check(got, a, b)
+        check(net.matmul8(a, b, out=c0.clone(), accumulate=True, workspace=ws[:size]), a, b, c0)
+        assert (ws[size:] == 255).all()
+        assert torch.equal(got, net.matmul8(a, b, dtype=dtype, workspace=ws[:size]))
+    wide = torch.full((m, n + 5), 3.0, dtype=dtype).cuda()
+    net.matmul8(a, b, out=wide[:, 1:1 + n])
+    check(wide[:, 1:1 + n], a, b)
+    assert (wide[:, :1] == 3).all() and (wide[:, 1 + n:] == 3).all()
+
+
+def test_parts_in_a_graph(net):
+    a, b = matrix(net, 70, 9000, 1, 23), matrix(net, 90, 9000, 1, 24)
+    graph = torch.cuda.CUDAGraph()
+    net.matmul8(a, b)
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        out = net.matmul8(a, b)
+    for i in range(3):
+        b.scales.view(torch.uint8).copy_(b.scales.view(torch.uint8).roll(1, 0))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out.clone(), net.matmul8(a, b))
+        torch.cuda.synchronize()
+
+
+def test_rows_of_scales_far_apart(net):
+    """Rows of scales at strides that do not fit the kernels' 32-bit offsets."""
+    m, n, k = 70, 2, 520
+    a, b = matrix(net, m, k, 1, 25), matrix(net, n, k, 1, 26)
+    far = torch.zeros((n - 1) * (1 << 32) + 8, dtype=torch.uint8, device="cuda").as_strided((n, 5), (1 << 32, 1))
+    far.copy_(b.scales.view(torch.uint8))
+    check(net.matmul8(a, net.Blocks8(b.values, far.view(torch.float8_e8m0fnu), 1), dtype=torch.float32), a, b)
+    check(net.matmul8(net.Blocks8(b.values, far.view(torch.float8_e8m0fnu), 1), a, dtype=torch.float32), b, a)
 
 
 def test_the_same_call_gives_the_same_bits(net):
