@@ -171,18 +171,34 @@ __device__ inline void block_products(f32x4 (&acc)[MI][NI], const uint32_t (&sa)
 #pragma unroll
     for (int j = 0; j < NI; j++) ok &= in_range(byte(sb[j]));
     const bool all = __all(ok);
-    Wide b[NI];
-#pragma unroll
-    for (int j = 0; j < NI; j++) b[j] = widen(get_b(j), all ? scale_of(byte(sb[j])) : 1.f);
     if (all) {
+      Wide a[2], b[NI];
+      b[0] = widen(get_b(0), scale_of(byte(sb[0])));
+      a[0] = widen(get_a(0), scale_of(byte(sa[0])));
 #pragma unroll
       for (int i = 0; i < MI; i++) {
-        const Wide a = widen(get_a(i), scale_of(byte(sa[i])));
 #pragma unroll
-        for (int j = 0; j < NI; j++) acc[i][j] = mfma16(b[j], a, acc[i][j]);
+        for (int j = 0; j < NI; j++) {
+          acc[i][j] = mfma16(b[j], a[i & 1], acc[i][j]);
+          if (i == 0 && j + 1 < NI) b[j + 1] = widen(get_b(j + 1), scale_of(byte(sb[j + 1])));
+        }
+        if (i + 1 < MI) a[(i + 1) & 1] = widen(get_a(i + 1), scale_of(byte(sa[i + 1])));
+      }
+      if constexpr (SPREAD) {  // operands are converted while the products of the ones before run
+        __builtin_amdgcn_sched_group_barrier(0x100, 8, 0);
+        __builtin_amdgcn_sched_group_barrier(0x2, 40, 0);
+#pragma unroll
+        for (int i = 0; i < MI * NI * 4; i++) {
+          __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+          __builtin_amdgcn_sched_group_barrier(0x2, 2, 0);
+          if (i % 4 == 1) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        }
       }
     } else {
       const int q4 = (threadIdx.x & 63) >> 4 << 2;
+      Wide b[NI];
+#pragma unroll
+      for (int j = 0; j < NI; j++) b[j] = widen(get_b(j), 1.f);
 #pragma unroll
       for (int i = 0; i < MI; i++) {
         const Wide a = widen(get_a(i), 1.f);
@@ -307,7 +323,9 @@ __global__ __launch_bounds__(64 * WM * WN, WM * WN * PER_CU / 4) void k_mm_tile(
   constexpr int W = WM * WN, MI = BM / WM / 16, NI = BN / WN / 16;
   constexpr int LA = BM / 8 / W, LB = BN / 8 / W;  // loads of 8 rows each by a wave
   static_assert(BM + BN <= 64 * W, "a thread for each row's scales");
-  __shared__ __attribute__((aligned(128))) uint8_t lds[2][(BM + BN) * 128];
+  // (An array for the even and one for the odd blocks: the compiler waits for loads into an LDS array before it reads that array.)
+  __shared__ __attribute__((aligned(128))) uint8_t lds0[(BM + BN) * 128], lds1[(BM + BN) * 128];
+  auto lds = [&](auto odd) -> uint8_t* { return odd == 0 ? lds0 : lds1; };
   __shared__ uint32_t four[2][BM + BN];
   const MatArgs g = my_part(whole);
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r16 = lane & 15, q = lane >> 4;
@@ -327,16 +345,16 @@ __global__ __launch_bounds__(64 * WM * WN, WM * WN * PER_CU / 4) void k_mm_tile(
   for (int j = 0; j < LA; j++) from_a[j] = (uint32_t)(min((j * W + wave) * 8 + (lane >> 3), rows_a)) * (uint32_t)g.a_stride + piece;
 #pragma unroll
   for (int j = 0; j < LB; j++) from_b[j] = (uint32_t)(min((j * W + wave) * 8 + (lane >> 3), rows_b)) * (uint32_t)g.b_stride + piece;
-  auto stage = [&](int kb, int to) {
+  auto stage = [&](int kb, auto to) {
     const uint8_t *pa = a0 + (int64_t)kb * 128, *pb = b0 + (int64_t)kb * 128;
 #pragma unroll
     for (int j = 0; j < LA; j++)
       __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(pa + from_a[j]),
-                                       (__attribute__((address_space(3))) void*)&lds[to][(j * W + wave) * 1024], 16, 0, 0);
+                                       (__attribute__((address_space(3))) void*)(lds(to) + (j * W + wave) * 1024), 16, 0, 0);
 #pragma unroll
     for (int j = 0; j < LB; j++)
       __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(pb + from_b[j]),
-                                       (__attribute__((address_space(3))) void*)&lds[to][BM * 128 + (j * W + wave) * 1024], 16, 0, 0);
+                                       (__attribute__((address_space(3))) void*)(lds(to) + BM * 128 + (j * W + wave) * 1024), 16, 0, 0);
   };
   // Scales: a thread has one of the tile's rows, asks for those of four blocks four blocks ahead and leaves them in LDS.
   const bool has_row = tid < BM + BN;
@@ -351,9 +369,9 @@ __global__ __launch_bounds__(64 * WM * WN, WM * WN * PER_CU / 4) void k_mm_tile(
   };
   f32x4 acc[MI][NI] = {};
   const int p0 = (q * 2 ^ mix(r16)) * 16, p1 = ((q * 2 + 1) ^ mix(r16)) * 16;
-  auto products = [&](int kb, int in) {
+  auto products = [&](int kb, auto in) {
     auto frag = [&](int row16) {
-      const uint8_t* at = &lds[in][(row16 + r16) * 128];
+      const uint8_t* at = lds(in) + (row16 + r16) * 128;
       const i32x4 lo = *(const i32x4*)(at + p0), hi = *(const i32x4*)(at + p1);
       return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
     };
@@ -371,24 +389,31 @@ __global__ __launch_bounds__(64 * WM * WN, WM * WN * PER_CU / 4) void k_mm_tile(
     if ((kb & 3) == 0 && kb + 4 < blocks) ask_scales(kb + 4);
   };
   if (has_row) four[0][tid] = load_scales(scales, 0, blocks);
-  if (direct > 0) stage(0, 0);
-  for (int kb = 0; kb < direct; kb++) {
+  constexpr Int<0> I0{};
+  constexpr Int<1> I1{};
+  if (direct > 0) stage(0, I0);
+  auto block = [&](int kb, auto odd) {
     __syncthreads();  // this block has landed, and the other half is free
     next_scales(kb);
-    if (kb + 1 < direct) stage(kb + 1, (kb + 1) & 1);
-    products(kb, kb & 1);
+    if (kb + 1 < direct) stage(kb + 1, Int<1 - odd>{});
+    products(kb, odd);
+  };
+#pragma unroll 1
+  for (int kb = 0; kb < direct; kb += 2) {
+    block(kb, I0);
+    if (kb + 1 < direct) block(kb + 1, I1);
   }
   for (int kb = direct; kb < blocks; kb++) {
     __syncthreads();
     for (int j = 0; j < LA; j++)
-      *(i32x4*)&lds[0][(j * W + wave) * 1024 + lane * 16] =
+      *(i32x4*)&lds0[(j * W + wave) * 1024 + lane * 16] =
           load16(a0 + (int64_t)min((j * W + wave) * 8 + (lane >> 3), rows_a) * g.a_stride, (int64_t)kb * 128 + piece, g.k);
     for (int j = 0; j < LB; j++)
-      *(i32x4*)&lds[0][BM * 128 + (j * W + wave) * 1024 + lane * 16] =
+      *(i32x4*)&lds0[BM * 128 + (j * W + wave) * 1024 + lane * 16] =
           load16(b0 + (int64_t)min((j * W + wave) * 8 + (lane >> 3), rows_b) * g.b_stride, (int64_t)kb * 128 + piece, g.k);
     next_scales(kb);
     __syncthreads();
-    products(kb, 0);
+    products(kb, I0);
   }
 #pragma unroll
   for (int i = 0; i < MI; i++)
