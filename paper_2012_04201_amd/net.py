@@ -183,6 +183,8 @@ def rms_norm_grad(dy, h, rstd, weight=None, dsum=None, want_dweight=True, worksp
             need = _SZ(0)
             _check(L.bbo_net_rms_norm_grad_workspace(rows, width, C.byref(need)))
             workspace = _room(stream, (max(need.value, 256),), (1,), torch.uint8, device)
+        elif workspace.device != device or not workspace.is_contiguous():
+            raise ValueError("workspace must be dense and on the same GPU")
         ws, room = workspace.data_ptr(), workspace.numel() * workspace.element_size()
     _check(L.bbo_net_rms_norm_grad(dy.data_ptr(), _row(dy), pd, d_stride, h.data_ptr(), _row(h), rstd.data_ptr(), pw, rows, width, _DTYPES[dtype],
                                    dx.data_ptr(), width, pg, ws, room, _stream(stream, h)))
@@ -235,6 +237,8 @@ def matmul8(a, b, dtype=torch.bfloat16, out=None, accumulate=False, workspace=No
         _check(L.bbo_net_matmul8_workspace(m, n, k, C.byref(need)))
         if need.value:
             workspace = _room(stream, (need.value,), (1,), torch.uint8, device)
+    elif workspace.device != device or not workspace.is_contiguous():
+        raise ValueError("workspace must be dense and on the same GPU")
     if workspace is not None:
         ws, room = workspace.data_ptr(), workspace.numel() * workspace.element_size()
     _check(L.bbo_net_matmul8(av.data_ptr(), _row(av), a.scales.data_ptr(), _row(a.scales), a.tile, bv.data_ptr(), _row(bv), b.scales.data_ptr(),

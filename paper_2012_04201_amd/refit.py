@@ -1,0 +1,158 @@
+"""A wide residual network on the searched data set, trained and served in 8 bits.
+
+After a search has found what the small models can do, this fits one wide network of the same kind of input to the same folds:
+an input layer, `blocks` times  h += relu(norm(h) w1^T) w2^T,  and a linear output of the normed h.  Every matrix product
+has both operands in 8 bits (forward pass, data gradient and weight gradient), the residual stream h is bfloat16, weights are
+float32 with 8-bit copies made anew after each step, and AdamW keeps its moments in 8 bits.
+
+    python -m paper_2012_04201_amd.refit --config 1 --width 1024 --hidden 2048 --blocks 2 --epochs 20
+"""
+import argparse
+import json
+import time
+
+import numpy as np
+import torch
+
+from . import net
+
+BF16 = torch.bfloat16
+
+
+class WideNetwork:
+    """A residual network for `inputs` features and `outputs` classes (or, with 1, a value).
+
+    step(x, y) trains on a batch, predict(x) serves one row or many.  x: bfloat16 [rows, inputs] on the GPU; y: int64
+    classes or float32 values."""
+
+    def __init__(self, inputs, outputs, width=1024, hidden=2048, blocks=2, lr=1e-3, weight_decay=0.01, seed=0, device="cuda"):
+        if min(inputs, outputs, width, hidden) < 1 or blocks < 0:
+            raise ValueError("inputs, outputs, width and hidden must be at least 1, blocks at least 0")
+        g = torch.Generator().manual_seed(seed)
+        draw = lambda n, k, scale=1.0: (torch.randn(n, k, generator=g) * scale * k ** -0.5).to(device)
+        self.outputs, self.blocks = outputs, blocks
+        # w[0]: inputs to h; w[2i + 1], w[2i + 2]: a block's; w[-1]: h to outputs
+        self.w = [draw(width, inputs)]
+        for _ in range(blocks):
+            self.w += [draw(hidden, width, 2 ** 0.5), draw(width, hidden, (blocks + 1) ** -0.5)]
+        self.w.append(draw(outputs, width))
+        self.norms = [torch.ones(width, device=device) for _ in range(blocks + 1)]
+        n = len(self.w) + len(self.norms)
+        self.optimizer = net.AdamW(self.w + self.norms, lr=lr, weight_decay=[weight_decay] * len(self.w) + [0.0] * (n - len(self.w)),
+                                   state="8bit", seed=seed)
+        self._weights()
+
+    def _weights(self):
+        """The weights in 8 bits, each by output (for the forward pass) and by input (for the data gradient)."""
+        pairs = [net.quantize(w, tile=128, want_cols=True) for w in self.w]
+        self.w8, self.w8t = [p[0] for p in pairs], [p[1] for p in pairs]
+
+    def predict(self, x):
+        """Logits (or values) float32 [rows, outputs]; the norm's output goes straight into 8 bits."""
+        h = net.matmul8(net.quantize(x)[0], self.w8[0])
+        n = net.rms_norm(h, self.norms[0], want_y=False, want_8bit=True)
+        for i in range(self.blocks):
+            u = net.matmul8(n.y8, self.w8[2 * i + 1])
+            o = net.matmul8(net.quantize(u, gate=u)[0], self.w8[2 * i + 2])
+            n = net.rms_norm(o, self.norms[i + 1], residual=h, want_y=False, want_8bit=True)
+            h = n.sum
+        return net.matmul8(n.y8, self.w8[-1], torch.float32)
+
+    def gradients(self, x, y):
+        """(loss, gradients of w and norms in their order) of a batch: cross entropy, or half the squared error."""
+        both = lambda t, gate=None: net.quantize(t, gate=gate, want_cols=True)
+        x8, x8t = both(x)
+        h = net.matmul8(x8, self.w8[0])
+        n = net.rms_norm(h, self.norms[0], want_rstd=True)
+        kept = []
+        for i in range(self.blocks):
+            y8, y8t = both(n.y)
+            u = net.matmul8(y8, self.w8[2 * i + 1])
+            r8, r8t = both(u, gate=u)
+            kept.append((h, n.rstd, y8t, u, r8t))
+            o = net.matmul8(r8, self.w8[2 * i + 2])
+            n = net.rms_norm(o, self.norms[i + 1], residual=h, want_rstd=True)
+            h = n.sum
+        y8, y8t = both(n.y)
+        out = net.matmul8(y8, self.w8[-1], torch.float32)
+        rows = x.shape[0]
+        if self.outputs > 1:
+            logp = torch.log_softmax(out, 1)
+            loss = -logp.gather(1, y[:, None]).mean()
+            d = logp.exp_().scatter_add_(1, y[:, None], torch.full_like(y[:, None], -1, dtype=torch.float32))
+        else:
+            d = out - y[:, None]
+            loss = d.square().mean() / 2
+        d8, d8t = both((d / rows).to(BF16))
+
+        dw, dnorm = [None] * len(self.w), [None] * len(self.norms)
+        dw[-1] = net.matmul8(d8t, y8t, torch.float32)
+        dh, dnorm[-1] = net.rms_norm_grad(net.matmul8(d8, self.w8t[-1]), h, n.rstd, self.norms[-1])
+        for i in reversed(range(self.blocks)):
+            h, rstd, y8t, u, r8t = kept[i]
+            d8, d8t = both(dh)
+            dw[2 * i + 2] = net.matmul8(d8t, r8t, torch.float32)
+            d8, d8t = both(net.matmul8(d8, self.w8t[2 * i + 2]), gate=u)
+            dw[2 * i + 1] = net.matmul8(d8t, y8t, torch.float32)
+            dh, dnorm[i] = net.rms_norm_grad(net.matmul8(d8, self.w8t[2 * i + 1]), h, rstd, self.norms[i], dsum=dh)
+        dw[0] = net.matmul8(net.quantize(dh, want_rows=False, want_cols=True)[1], x8t, torch.float32)
+        return loss, dw + dnorm
+
+    def step(self, x, y):
+        """One step of AdamW on a batch; its loss before the step, on the GPU."""
+        loss, grads = self.gradients(x, y)
+        self.optimizer.step(grads)
+        self._weights()
+        return loss
+
+
+def refit(cfg, width=1024, hidden=2048, blocks=2, epochs=20, batch=512, lr=1e-3, weight_decay=0.01, seed=0, held_out=0):
+    """Fits a WideNetwork to a workload's rows outside fold `held_out`; (network, record of what came of it)."""
+    X = torch.from_numpy(np.ascontiguousarray(cfg["X"], dtype=np.float32)).to("cuda", BF16)
+    classes = cfg["n_classes"] >= 2
+    y = torch.from_numpy(np.asarray(cfg["y"], dtype=np.int64 if classes else np.float32)).cuda()
+    out = torch.from_numpy(np.asarray(cfg["fold_idx"]) == held_out).cuda()
+    Xt, yt, Xv, yv = X[~out].contiguous(), y[~out], X[out].contiguous(), y[out]
+    model = WideNetwork(X.shape[1], cfg["n_classes"] if classes else 1, width, hidden, blocks, lr, weight_decay, seed)
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    losses, steps = [], 0
+    torch.cuda.synchronize()
+    start = time.perf_counter()
+    for _ in range(epochs):
+        order = torch.randperm(len(yt), generator=g, device="cuda")
+        total = torch.zeros((), device="cuda")
+        for at in range(0, len(yt), batch):
+            rows = order[at:at + batch]
+            total += model.step(Xt[rows], yt[rows]) * len(rows)
+            steps += 1
+        losses.append(total / len(yt))
+    losses = torch.stack(losses).tolist() if losses else []
+    seconds = time.perf_counter() - start
+    p = model.predict(Xv)
+    score = (p.argmax(1) == yv).float().mean() if classes else -(p[:, 0] - yv).square().mean()
+    row = Xv[:1].contiguous()
+    model.predict(row)
+    torch.cuda.synchronize()
+    start = time.perf_counter()
+    for _ in range(20):
+        model.predict(row)
+    torch.cuda.synchronize()
+    return model, {"rows": len(yt), "steps": steps, "loss": losses, "score": float(score), "ms_per_step": 1e3 * seconds / max(steps, 1),
+                   "us_per_served_row": (time.perf_counter() - start) / 20 * 1e6}
+
+
+def main():
+    from . import inputs
+    ap = argparse.ArgumentParser(description=__doc__.split("\n")[0])
+    ap.add_argument("--config", type=int, default=1, help="workload of inputs.make_config")
+    for name, value in (("width", 1024), ("hidden", 2048), ("blocks", 2), ("epochs", 20), ("batch", 512), ("seed", 0)):
+        ap.add_argument("--" + name, type=int, default=value)
+    ap.add_argument("--lr", type=float, default=1e-3)
+    a = ap.parse_args()
+    cfg = inputs.make_config(a.config, B=1)
+    _, record = refit(cfg, a.width, a.hidden, a.blocks, a.epochs, a.batch, a.lr, seed=a.seed)
+    print(json.dumps({"workload": cfg["name"], **{k: v for k, v in record.items() if k != "loss"}, "first_loss": record["loss"][0], "last_loss": record["loss"][-1]}))
+
+
+if __name__ == "__main__":
+    main()
