@@ -211,9 +211,14 @@ __global__ __launch_bounds__(1024) void k_dweight(const float* parts, int shares
   }
 }
 
-// The cut by the width: as few threads as hold the row in registers.
+// The cut by the width: as few threads as hold the row in registers.  waves (of a gradient): a wave takes a row up to 2048 columns, not
+// to 1024 (a wave has no meeting with others and no idle half where the width is just past 1024, but fewer rows are on their way).
 template <typename E, template <typename, int, int, bool> class F, bool WHOLE, typename A>
-void cut(int width, const A& a, hipStream_t s) {
+void cut(int width, bool waves, const A& a, hipStream_t s) {
+  if constexpr (F<E, 64, 1, WHOLE>::GRADIENT) {
+    if (waves && width > 1536) return F<E, 64, 4, WHOLE>::go(a, s);
+    if (waves && width > 1024) return F<E, 64, 3, WHOLE>::go(a, s);
+  }
   if (width <= 512) F<E, 64, 1, WHOLE>::go(a, s);
   else if (width <= 1024) F<E, 64, 2, WHOLE>::go(a, s);
   else if (width <= 2048) F<E, 256, 1, WHOLE>::go(a, s);
@@ -223,12 +228,13 @@ void cut(int width, const A& a, hipStream_t s) {
   else F<E, 1024, 4, WHOLE>::go(a, s);
 }
 template <typename E, template <typename, int, int, bool> class F, typename A>
-void by_width(int width, const A& a, hipStream_t s) {
-  if (width % 8 == 0) cut<E, F, true>(width, a, s);
-  else cut<E, F, false>(width, a, s);
+void by_width(int width, bool waves, const A& a, hipStream_t s) {
+  if (width % 8 == 0) cut<E, F, true>(width, waves, a, s);
+  else cut<E, F, false>(width, waves, a, s);
 }
 template <typename E, int T, int NV, bool WHOLE>
 struct Norm {
+  static constexpr bool GRADIENT = false;
   static void go(const NormArgs& a, hipStream_t s) {
     using C = RowCut<T, NV>;
     hipLaunchKernelGGL((k_rms_norm<E, T, NV, WHOLE>), dim3((uint32_t)ceil_div(a.rows, C::PER_WG)), dim3(C::THREADS), 0, s, a);
@@ -236,22 +242,26 @@ struct Norm {
 };
 template <typename E, int T, int NV, bool WHOLE>
 struct Grad {
+  static constexpr bool GRADIENT = true;
   static void go(const GradArgs& a, hipStream_t s) {
     using C = RowCut<T, NV>;
     hipLaunchKernelGGL((k_rms_norm_grad<E, T, NV, WHOLE>), dim3((uint32_t)ceil_div(a.groups, C::PER_WG)), dim3(C::THREADS), 0, s, a);
   }
 };
 
-// Groups of threads that share the rows of a gradient: a wave each up to 1024 columns, a workgroup beyond; up to four to eight workgroups of
+// The gradient of many rows: a wave a row up to 2048 columns (us, a wave against a workgroup: 20000 x 1111 in bfloat16 60 / 82, x 1536 51 /
+// 57, x 2048 68 / 75, in float32 84 / 88, 98 / 105, 129 / 136; 1797 x 1111 in float32 17.0 / 16.3, one row of 2048 7.7 / 6.7).
+bool grad_waves(int64_t rows, int64_t width) { return width <= 1024 || (width <= 2048 && rows >= 4096); }
+// Groups of threads that share the rows of a gradient: a wave each, or a workgroup; up to four to eight workgroups of
 // 256 threads a CU; with four rows each at least where that leaves two to four workgroups a CU (a share of dweight costs as much as half a row).
 int grad_groups(int64_t rows, int64_t width) {
-  const int most = width <= 1024 ? 4096 : width <= 2048 ? 2048 : width <= 8192 ? 1024 : 512;
+  const int most = grad_waves(rows, width) ? 4096 : width <= 2048 ? 2048 : width <= 8192 ? 1024 : 512;
   const int64_t few = width <= 2048 ? 1024 : 512, by_four = rows / 4 > few ? rows / 4 : rows < few ? rows : few;
   return (int)(by_four < most ? by_four : most);
 }
 int grad_shares(int64_t rows, int64_t width) {
   const int groups = grad_groups(rows, width);
-  return width <= 1024 ? (groups + 3) / 4 : groups;
+  return grad_waves(rows, width) ? (groups + 3) / 4 : groups;
 }
 
 int check_rows(int64_t rows, int64_t width, int32_t dtype) {
@@ -283,8 +293,11 @@ int bbo_net_rms_norm(const void* x, int64_t x_stride, const void* residual, int6
     return net_fail(BBO_INVALID_ARG, "a stride is less than a row");
   const NormArgs a{x, residual, weight, sum, y, rstd, (uint8_t*)q, (uint8_t*)q_scales, x_stride, residual_stride, sum_stride,
                    y_stride, q_stride, q_scale_stride, rows, (int)width, eps};
-  if (dtype == BBO_F32) by_width<float, Norm>((int)width, a, (hipStream_t)stream);
-  else by_width<bf16, Norm>((int)width, a, (hipStream_t)stream);
+  // (us, a wave a row against a workgroup: 20000 x 1111 in bfloat16 39 / 49, but x 1536 45 / 42, 1797 x 1111 9.4 / 7.3, 20000 x 1111 in float32
+  // 80 / 73: only where the rows are many, short and end in the middle of a vector)
+  if (dtype == BBO_F32) by_width<float, Norm>((int)width, false, a, (hipStream_t)stream);
+  else if (rows >= 4096 && width > 1024 && width <= 1536 && width % 8) Norm<bf16, 64, 3, false>::go(a, (hipStream_t)stream);
+  else by_width<bf16, Norm>((int)width, false, a, (hipStream_t)stream);
   return net_launched();
 }
 
@@ -313,8 +326,9 @@ int bbo_net_rms_norm_grad(const void* dy, int64_t dy_stride, const void* dsum, i
       return net_fail(BBO_WORKSPACE_TOO_SMALL, "workspace too small");
     const GradArgs a{dy, dsum, h, rstd, weight, dx, dweight ? (float*)workspace : nullptr, dy_stride, dsum_stride, h_stride,
                      dx_stride, rows, (int)width, groups};
-    if (dtype == BBO_F32) by_width<float, Grad>((int)width, a, s);
-    else by_width<bf16, Grad>((int)width, a, s);
+    const bool waves = grad_waves(rows, width);
+    if (dtype == BBO_F32) by_width<float, Grad>((int)width, waves, a, s);
+    else by_width<bf16, Grad>((int)width, waves, a, s);
     if (int rc = net_launched()) return rc;
   }
   if (dweight) {

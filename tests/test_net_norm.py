@@ -51,7 +51,10 @@ SHAPES = [(1, 1), (3, 7), (1, 1024), (5, 129), (33, 512), (70, 513), (17, 1024),
           (2, 16384), (2, 20001), (1, 32768)]
 
 
-@pytest.mark.parametrize("rows,width", SHAPES)
+MANY = [(4099, 1025), (4098, 1111), (4097, 1536), (4096, 2041), (4100, 2048)]  # a wave takes a row
+
+
+@pytest.mark.parametrize("rows,width", SHAPES + MANY[:2])
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 @pytest.mark.parametrize("residual", [False, True])
 def test_norm(net, rows, width, dtype, residual):
@@ -73,7 +76,7 @@ def test_norm(net, rows, width, dtype, residual):
     check_y8(g.y8, O.rms_norm(h.double(), torch.ones(width).double(), EPS))
 
 
-@pytest.mark.parametrize("rows,width", SHAPES + [(700, 100), (3000, 70)])
+@pytest.mark.parametrize("rows,width", SHAPES + [(700, 100), (3000, 70)] + MANY)
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 @pytest.mark.parametrize("dsum", [False, True])
 def test_gradient(net, rows, width, dtype, dsum):
