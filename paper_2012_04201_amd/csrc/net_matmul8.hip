@@ -140,9 +140,9 @@ __device__ inline void put4(const MatArgs& g, int64_t m, int64_t n, f32x4 v) {
 }
 
 // Products of one block of 128 for MI x NI tiles of 16 x 16, added to acc.  get_a(i), get_b(j): a lane's 32 codes of a row;
-// sa, sb: the rows' scales, in byte U.
+// sa, sb: the rows' scales, in byte U.  SPREAD and EXACT: as the bits of float32, and `fast` says whether all are in range.
 template <bool EXACT, int U, bool SPREAD, int MI, int NI, typename A, typename B>
-__device__ inline void block_products(f32x4 (&acc)[MI][NI], const uint32_t (&sa)[MI], const uint32_t (&sb)[NI], A get_a, B get_b) {
+__device__ inline void block_products(f32x4 (&acc)[MI][NI], const uint32_t (&sa)[MI], const uint32_t (&sb)[NI], A get_a, B get_b, bool fast = false) {
   if constexpr (!EXACT) {
     i32x8 b[NI];
 #pragma unroll
@@ -164,25 +164,29 @@ __device__ inline void block_products(f32x4 (&acc)[MI][NI], const uint32_t (&sa)
       }
     }
   } else {
-    auto byte = [](uint32_t s) { return (int)(s >> (8 * U) & 255); };
-    bool ok = true;
+    auto byte = [](uint32_t s) { return (int)(SPREAD ? s >> 23 : s >> (8 * U) & 255); };
+    auto power = [&](uint32_t s) { return as_f32(SPREAD ? s : (uint32_t)byte(s) << 23); };  // of a byte in range
+    bool all = fast;
+    if constexpr (!SPREAD) {
+      bool ok = true;
 #pragma unroll
-    for (int i = 0; i < MI; i++) ok &= in_range(byte(sa[i]));
+      for (int i = 0; i < MI; i++) ok &= in_range(byte(sa[i]));
 #pragma unroll
-    for (int j = 0; j < NI; j++) ok &= in_range(byte(sb[j]));
-    const bool all = __all(ok);
+      for (int j = 0; j < NI; j++) ok &= in_range(byte(sb[j]));
+      all = __all(ok);
+    }
     if (all) {
       Wide a[2], b[NI];
-      b[0] = widen(get_b(0), scale_of(byte(sb[0])));
-      a[0] = widen(get_a(0), scale_of(byte(sa[0])));
+      b[0] = widen(get_b(0), power(sb[0]));
+      a[0] = widen(get_a(0), power(sa[0]));
 #pragma unroll
       for (int i = 0; i < MI; i++) {
 #pragma unroll
         for (int j = 0; j < NI; j++) {
           acc[i][j] = mfma16(b[j], a[i & 1], acc[i][j]);
-          if (i == 0 && j + 1 < NI) b[j + 1] = widen(get_b(j + 1), scale_of(byte(sb[j + 1])));
+          if (i == 0 && j + 1 < NI) b[j + 1] = widen(get_b(j + 1), power(sb[j + 1]));
         }
-        if (i + 1 < MI) a[(i + 1) & 1] = widen(get_a(i + 1), scale_of(byte(sa[i + 1])));
+        if (i + 1 < MI) a[(i + 1) & 1] = widen(get_a(i + 1), power(sa[i + 1]));
       }
       if constexpr (SPREAD) {  // operands are converted while the products of the ones before run
         __builtin_amdgcn_sched_group_barrier(0x100, 8, 0);
@@ -326,7 +330,8 @@ __global__ __launch_bounds__(64 * WM * WN, WM * WN * PER_CU / 4) void k_mm_tile(
   // (An array for the even and one for the odd blocks: the compiler waits for loads into an LDS array before it reads that array.)
   __shared__ __attribute__((aligned(128))) uint8_t lds0[(BM + BN) * 128], lds1[(BM + BN) * 128];
   auto lds = [&](auto odd) -> uint8_t* { return odd == 0 ? lds0 : lds1; };
-  __shared__ uint32_t four[2][BM + BN];
+  __shared__ uint32_t scale[8][BM + BN];  // of block kb in [kb & 7], as block_products() wants them
+  __shared__ int range[2][W];             // EXACT, of four blocks: whether a wave's rows have all of theirs in range
   const MatArgs g = my_part(whole);
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r16 = lane & 15, q = lane >> 4;
   const int wm = wave / WN * (BM / WM), wn = wave % WN * (BN / WN);
@@ -364,9 +369,22 @@ __global__ __launch_bounds__(64 * WM * WN, WM * WN * PER_CU / 4) void k_mm_tile(
   auto ask_scales = [&](int kb) {  // (4 <= kb < blocks; the row's last four where fewer than four follow)
     if (has_row) next = *(const u32_any*)(scales + min(kb, blocks - 4));
   };
-  auto keep_scales = [&](int kb) {  // of the four blocks from kb on
-    if (has_row) four[kb >> 2 & 1][tid] = next >> (8 * (kb - min(kb, blocks - 4)));
+  auto keep_scales = [&](int kb, uint32_t from) {  // of the four blocks from kb on
+    bool ok = true;
+    if (has_row) {
+#pragma unroll
+      for (int i = 0; i < 4; i++) {
+        const uint32_t byte = from >> (8 * i) & 255;
+        scale[(kb & 4) + i][tid] = EXACT ? byte << 23 : byte;
+        ok &= kb + i >= blocks || in_range((int)byte);
+      }
+    }
+    if constexpr (EXACT) {
+      ok = __all(ok);
+      if (lane == 0) range[kb >> 2 & 1][wave] = ok;
+    }
   };
+  bool fast = true;  // in these four blocks
   f32x4 acc[MI][NI] = {};
   const int p0 = (q * 2 ^ mix(r16)) * 16, p1 = ((q * 2 + 1) ^ mix(r16)) * 16;
   auto products = [&](int kb, auto in) {
@@ -375,20 +393,26 @@ __global__ __launch_bounds__(64 * WM * WN, WM * WN * PER_CU / 4) void k_mm_tile(
       const i32x4 lo = *(const i32x4*)(at + p0), hi = *(const i32x4*)(at + p1);
       return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
     };
-    const uint8_t* s = (const uint8_t*)&four[kb >> 2 & 1][r16] + (kb & 3);
+    const uint32_t* from = &scale[kb & 7][r16];
     uint32_t sa[MI], sb[NI];
 #pragma unroll
-    for (int i = 0; i < MI; i++) sa[i] = s[(wm + i * 16) * 4];
+    for (int i = 0; i < MI; i++) sa[i] = from[wm + i * 16];
 #pragma unroll
-    for (int i = 0; i < NI; i++) sb[i] = s[(BM + wn + i * 16) * 4];
-    block_products<EXACT, 0, true, MI, NI>(acc, sa, sb, [&](int i) { return frag(wm + i * 16); }, [&](int j) { return frag(BM + wn + j * 16); });
+    for (int i = 0; i < NI; i++) sb[i] = from[BM + wn + i * 16];
+    if (EXACT && (kb & 3) == 0) {
+      int all = 1;
+#pragma unroll
+      for (int i = 0; i < W; i++) all &= range[kb >> 2 & 1][i];
+      fast = __builtin_amdgcn_readfirstlane(all) != 0;
+    }
+    block_products<EXACT, 0, true, MI, NI>(acc, sa, sb, [&](int i) { return frag(wm + i * 16); }, [&](int j) { return frag(BM + wn + j * 16); }, fast);
   };
   // (block kb's scales were kept in block kb - 1 or before; what block kb - 1 read is free)
   auto next_scales = [&](int kb) {
-    if ((kb & 3) == 3 && kb + 1 < blocks) keep_scales(kb + 1);
+    if ((kb & 3) == 3 && kb + 1 < blocks) keep_scales(kb + 1, next >> (8 * (kb + 1 - min(kb + 1, blocks - 4))));
     if ((kb & 3) == 0 && kb + 4 < blocks) ask_scales(kb + 4);
   };
-  if (has_row) four[0][tid] = load_scales(scales, 0, blocks);
+  keep_scales(0, has_row ? load_scales(scales, 0, blocks) : 0);
   constexpr Int<0> I0{};
   constexpr Int<1> I1{};
   if (direct > 0) stage(0, I0);
