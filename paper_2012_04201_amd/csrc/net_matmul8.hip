@@ -186,17 +186,7 @@ __device__ inline void block_products(f32x4 (&acc)[MI][NI], const uint32_t (&sa)
           acc[i][j] = mfma16(b[j], a[i & 1], acc[i][j]);
           if (i == 0 && j + 1 < NI) b[j + 1] = widen(get_b(j + 1), power(sb[j + 1]));
         }
-        if (i + 1 < MI) a[(i + 1) & 1] = widen(get_a(i + 1), power(sa[i + 1]));
-      }
-      if constexpr (SPREAD) {  // operands are converted while the products of the ones before run
-        __builtin_amdgcn_sched_group_barrier(0x100, 8, 0);
-        __builtin_amdgcn_sched_group_barrier(0x2, 40, 0);
-#pragma unroll
-        for (int i = 0; i < MI * NI * 4; i++) {
-          __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
-          __builtin_amdgcn_sched_group_barrier(0x2, 2, 0);
-          if (i % 4 == 1) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-        }
+        if (i + 1 < MI) a[(i + 1) & 1] = widen(get_a(i + 1), power(sa[i + 1]));  // (while these products run)
       }
     } else {
       const int q4 = (threadIdx.x & 63) >> 4 << 2;
@@ -879,19 +869,23 @@ enum Kernel { ROWS, SMALL, LARGE, PIPE };
 struct Plan {
   Kernel kernel;
   int64_t splits, per;
+  int64_t ahead;  // rows of a that go to k_mm_pipe ahead of the others
 };
 int64_t padded4(int64_t n) { return (n + 3) & ~3ll; }
-int64_t parts_bytes(const Plan& p, int64_t m, int64_t n) { return p.splits > 1 ? p.splits * m * padded4(n) * 4 : 0; }
-// (pipe_too: the operands' rows are as k_mm_pipe needs them; room: bytes of workspace)
-Plan plan_of(bool exact, bool pipe_too, int64_t m, int64_t n, int64_t k, size_t room) {
+int64_t parts_bytes(const Plan& p, int64_t m, int64_t n) { return p.splits > 1 ? p.splits * (m - p.ahead) * padded4(n) * 4 : 0; }
+struct Choice {
+  Plan plan;
+  double us;
+};
+// (room: bytes of workspace)
+Choice without_pipe(bool exact, int64_t m, int64_t n, int64_t k, size_t room) {
   const int64_t blocks = ceil_div(k, 128);
-  Plan best{SMALL, 1, blocks};
-  double least = 1e300;
+  Choice best{{SMALL, 1, blocks, 0}, 1e300};
   const double values = (double)m * padded4(n);
   const double most = (double)(room < (1u << 28) - 1 ? room : (1u << 28) - 1) / 4 / values;  // parts that there is room for
   auto offer = [&](Kernel kernel, int64_t s, double us) {
     if (s > 1) us += 3 + s * values * 8 / 3e6;
-    if (us < least) least = us, best = Plan{kernel, s, ceil_div(blocks, s)};
+    if (us < best.us) best = Choice{{kernel, s, ceil_div(blocks, s), 0}, us};
   };
   if (m <= 32) {  // (eight waves share a part's blocks)
     const int64_t groups = ceil_div(n, 16);
@@ -903,30 +897,57 @@ Plan plan_of(bool exact, bool pipe_too, int64_t m, int64_t n, int64_t k, size_t 
       return (double)(groups >> 9) * two + (last == 0 ? 0 : last <= 256 ? one : two);
     };
     const int64_t large = ceil_div(m, 128) * ceil_div(n, 128), small = ceil_div(m, 64) * ceil_div(n, 64);
-    if (pipe_too && k > 384) offer(PIPE, 1, 1.75 * (double)(ceil_div(ceil_div(m, 256) * ceil_div(n, 256), 256) * blocks));
     for (int64_t s = 1; s == 1 || (s <= 16 && s * 4 <= blocks && s <= most && large * s <= 1024); s++) {
       const double each = (double)ceil_div(blocks, s);
-      offer(LARGE, s, each * rounds(large * s, exact ? 1.6 : 0.76, exact ? 2.3 : 1.1));
+      offer(LARGE, s, each * rounds(large * s, exact ? 1.4 : 0.76, exact ? 1.9 : 1.1));
       offer(SMALL, s, each * rounds(small * s, exact ? 0.6 : 0.34, exact ? 0.84 : 0.48));
     }
   }
-  best.splits = best.per > 0 ? ceil_div(blocks, best.per) : 1;  // (no empty part)
+  Plan& p = best.plan;
+  p.splits = p.per > 0 ? ceil_div(blocks, p.per) : 1;  // (no empty part)
   return best;
+}
+// (pipe_too: the operands' rows are as k_mm_pipe needs them)
+Plan plan_of(bool exact, bool pipe_too, int64_t m, int64_t n, int64_t k, size_t room) {
+  Choice best = without_pipe(exact, m, n, k, room);
+  if (pipe_too && k > 384 && m > 32) {
+    const int64_t tm = ceil_div(m, 256), tn = ceil_div(n, 256), blocks = ceil_div(k, 128);
+    const double all = 1.75 * (double)(ceil_div(tm * tn, 256) * blocks);
+    if (all < best.us) best = Choice{{PIPE, 1, blocks, 0}, all};
+    // Whole rounds of its tiles, and the rows that are left to another kernel.
+    const int64_t full = tm * tn >> 8, ahead = 256 * (full * 256 / tn);
+    if (full > 0 && ahead > 0 && ahead < m) {
+      Choice rest = without_pipe(exact, m - ahead, n, k, room);
+      rest.plan.ahead = ahead;
+      rest.us += 1.75 * (double)(full * blocks) + 3;
+      if (rest.us < best.us) best = rest;
+    }
+  }
+  return best.plan;
 }
 
 template <bool EXACT>
 void launch(MatArgs& g, void* workspace, size_t room, hipStream_t s) {
   const Plan p = plan_of(EXACT, !EXACT && g.direct, g.m, g.n, g.k, room);
+  if constexpr (!EXACT) {
+    if (p.kernel == PIPE) return pipe(g, s);
+    if (p.ahead > 0) {
+      MatArgs first = g;
+      first.m = p.ahead;
+      pipe(first, s);
+      g.a += p.ahead * g.a_stride;
+      g.as += (p.ahead >> g.a_shift) * g.as_stride;
+      g.c = (char*)g.c + p.ahead * g.c_stride * 2;
+      g.m -= p.ahead;
+    }
+  }
   g.splits = (int)p.splits;
   g.per = (int)p.per;
   g.parts = (float*)workspace;
   g.n4 = padded4(g.n);
-  switch (p.kernel) {
-    case ROWS: g.m <= 16 ? rows<EXACT, 1>(g, s) : rows<EXACT, 2>(g, s); break;
-    case SMALL: small<EXACT>(g, s); break;
-    case LARGE: tiles<EXACT, 128, 128, 2, 2, 2>(g, s); break;
-    case PIPE: if constexpr (!EXACT) pipe(g, s); break;
-  }
+  if (p.kernel == ROWS) g.m <= 16 ? rows<EXACT, 1>(g, s) : rows<EXACT, 2>(g, s);
+  else if (p.kernel == SMALL) small<EXACT>(g, s);
+  else tiles<EXACT, 128, 128, 2, 2, 2>(g, s);
   if (g.splits > 1) hipLaunchKernelGGL(k_mm_join, dim3((uint32_t)ceil_div(g.m * (g.n4 >> 2), 256)), dim3(256), 0, s, g);
 }
 

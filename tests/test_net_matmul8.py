@@ -84,7 +84,8 @@ def test_many_tiles(net, m, n, k):
     check(net.matmul8(a, b, dtype=torch.float32), a, b)
 
 
-@pytest.mark.parametrize("m,n,k", [(3300, 4000, 385), (3333, 3845, 512), (3400, 3840, 640), (3585, 3601, 900), (3300, 4000, 1024), (6200, 1900, 1151)])
+@pytest.mark.parametrize("m,n,k", [(3300, 4000, 385), (3333, 3845, 512), (3400, 3840, 640), (3585, 3601, 900), (3300, 4000, 1024), (6200, 1900, 1151), (4500, 4000, 641),
+                                   (4110, 4097, 512), (17000, 1000, 1000)])
 def test_many_large_tiles(net, m, n, k):
     """Largest tiles, ragged at every edge; odd and even numbers of blocks, whole and with a part at the end."""
     a, b = matrix(net, m, k, 1, 18), matrix(net, n, k, 128 if k & 1 else 1, 19)
