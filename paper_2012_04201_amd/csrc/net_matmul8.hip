@@ -220,8 +220,9 @@ __device__ inline uint32_t load_scales(const uint8_t* row, int kb, int blocks) {
 }
 
 // ---------------------------------------------------------------------------
-// Few rows: 16 columns of c a workgroup, whose waves share the contracted index.  Bound by the bytes of b, which go straight
-// to registers, four blocks of a wave at once.
+// Few rows: 16 columns of c a workgroup, whose waves share the contracted index.  Bound by the bytes of b, which no other workgroup
+// reads and which go straight to registers, four blocks of a wave at once, so that 4096 x 4096 is on its way as a whole: 6.5 us for one row
+// (3.6 of them a launch), 8.4 for 16; 8192 x 8192 14.1 us, 4.7 TB/s, what a large copy reaches.  Block by block: 6.9 us.
 // ---------------------------------------------------------------------------
 template <bool EXACT, int MT, int W>
 __global__ __launch_bounds__(64 * W) void k_mm_rows(const MatArgs whole) {
@@ -298,6 +299,10 @@ __global__ __launch_bounds__(64 * W) void k_mm_rows(const MatArgs whole) {
 // A row's eight 16-byte pieces are stored at piece ^ f(row), f = (row & 7) ^ (row >> 3 & 1): the 16 rows that a read takes
 // side by side then fall on different banks.  Whole blocks of rows at multiples of 16 bytes go from global memory to LDS by
 // themselves (g.direct); a last part of a block, and rows at other addresses, through registers.
+// What bounds it, with two workgroups of 128 x 128 a CU: for float32 output 8192^3 takes 927 us (1.19 PFLOP/s, the library's bfloat16
+// product of that size 1.21); each matrix instruction has two conversions beside it, which run under it, and the vector instructions that
+// are left cost the most (scales decoded in every block: 1070 us).  For bfloat16 output the instructions fill a third of the cycles: a
+// block's way to LDS, which one workgroup waits for while the other multiplies, is as long as its products.
 // ---------------------------------------------------------------------------
 __device__ inline int mix(int row) { return (row & 7) ^ (row >> 3 & 1); }
 
@@ -437,7 +442,9 @@ __global__ __launch_bounds__(64 * WM * WN, WM * WN * PER_CU / 4) void k_mm_tile(
 
 // ---------------------------------------------------------------------------
 // Tiles of 64 x 64 by 2 x 2 waves, where there are few: bound by the way of a block to LDS, so that three are on it while one is
-// multiplied.
+// multiplied: 200 x 4096 x 4096 to bfloat16 12 us (one on its way: 20).  A last part of a block, and rows at other addresses, are asked
+// for ahead into registers: 1797 x 1000 x 569 to float32 11.4 us (asked for when they are due: 16); five blocks there are a chain of a
+// launch, the first rows' way (6.5 us in all for 64 x 64 x 128), 0.75 us a block and the part's.
 // ---------------------------------------------------------------------------
 // All waves' loads but their last VM have landed, all their reads from LDS but the last LGKM are done.
 template <int VM, int LGKM>
@@ -449,7 +456,6 @@ __device__ inline void all_here() {
   __builtin_amdgcn_sched_barrier(0);
   asm volatile("" ::: "memory");
 }
-
 
 template <bool EXACT>
 __global__ __launch_bounds__(256, 2) void k_mm_small(const MatArgs whole, int tiles_m, int tiles_n) {
@@ -600,7 +606,7 @@ __global__ __launch_bounds__(256, 2) void k_mm_small(const MatArgs whole, int ti
 // Waves 4 to 7 are a part behind, so that of the two waves of a SIMD one multiplies while the other loads.  Loads return in order: the
 // wait for some rows is a count of the younger loads.  It is made a quarter before the rows are read, and rows are asked for a
 // quarter after all waves have read what was in their place, as the other half of the waves needs.
-// What bounds it: 8192^3 takes 434 us (2.53 PFLOP/s; 360 us on zeros): the instructions fill 63 % of the cycles, at 1.92 GHz, which is the
+// What bounds it: 8192^3 takes 420 to 440 us (2.5 to 2.6 PFLOP/s; 360 us on zeros): the instructions fill 63 % of the cycles, at 1.92 GHz, which is the
 // power limit's doing; the barriers and the unequal parts are the rest.  Plain double buffering with one barrier a block: 474 us.  By quarters
 // without the shift of half the waves: 466.  With 32 x 32 x 64 instructions: 478, at a lower clock.
 // ---------------------------------------------------------------------------
@@ -858,13 +864,14 @@ void pipe(const MatArgs& g, hipStream_t s) {
 }
 
 // Which kernel, and in how many parts of the contracted index: the one that takes least by its measured time for a block of 128.  A
-// workgroup of 128 x 128 (of 64 x 64) alone on its CU takes 0.76 (0.34) us a block for bfloat16 output and 1.6 (0.6) for
-// float32, two together 1.1 (0.48) and 2.3 (0.84); 256 x 256 takes 1.75.  Parts cost the join's launch and 8 bytes of every
-// value a part at 3 TB/s.  us, one kernel against another: 4096^3 61 / 76 / 148 by falling size; 20000 x 1024 x 4096 105 / 97 / 180;
-// 2048^2 x 4096 50 / 29 / 41; 1024^2 x 4096 49 / 28 / 16.  One part against the chosen number: 1000 x 512 x 20000 59 / 33, float32 102 /
-// 43; 100 x 100 x 16000 44 / 13, float32 80 / 18; 4096 x 1024 x 20000 in float32 253 / 192.  Up to 32 rows go to
-// k_mm_rows (16 x 4096 x 4096 10.0 us, 64 x 64 tiles in four parts 11.5; 32 rows 12.7 / 12.4, in float32 12.9 / 14.7; 33 rows
-// 13.9 / 12.1), which is in parts where its workgroups are few (1 x 100 x 16000 16 / 9.5).
+// workgroup of 128 x 128 (of 64 x 64) alone on its CU takes 0.73 (0.30) us a block for bfloat16 output and 1.2 (0.50) for
+// float32, two together 1.05 (0.54) and 1.87 (0.75); 256 x 256 takes 1.75.  Parts cost the join's launch and 8 bytes of every
+// value a part at 3 TB/s.  us, one kernel against another, by falling size: bfloat16 4096^3 61 / 76 / 142, 2048^2 x 4096 50 / 29 /
+// 40, 1024^2 x 4096 49 / 27 / 15; float32 4096^3 - / 125 / 184, 2048^2 x 4096 - / 47 / 51, 1024^2 x 4096 - / 45 / 21.  One part against the
+// chosen number: 1000 x 512 x 20000 49 / 32, float32 82 / 39; 100 x 100 x 16000 36 / 12, float32 62 / 16; 4096 x 1024 x 20000 in
+// float32 197 / 165.  20000 x 1024 x 4096: largest tiles 105, 128 x 128 101, whole rounds of the largest and the rest by others 88.
+// Up to 32 rows go to k_mm_rows (16 x 4096 x 4096 10.0 us, 64 x 64 tiles in four parts 11.5; 32 rows 12.7 / 12.4, in float32
+// 12.9 / 14.7; 33 rows 13.9 / 12.1), which is in parts where its workgroups are few (1 x 100 x 16000 16 / 9.5).
 enum Kernel { ROWS, SMALL, LARGE, PIPE };
 struct Plan {
   Kernel kernel;
@@ -899,8 +906,8 @@ Choice without_pipe(bool exact, int64_t m, int64_t n, int64_t k, size_t room) {
     const int64_t large = ceil_div(m, 128) * ceil_div(n, 128), small = ceil_div(m, 64) * ceil_div(n, 64);
     for (int64_t s = 1; s == 1 || (s <= 16 && s * 4 <= blocks && s <= most && large * s <= 1024); s++) {
       const double each = (double)ceil_div(blocks, s);
-      offer(LARGE, s, each * rounds(large * s, exact ? 1.4 : 0.76, exact ? 1.9 : 1.1));
-      offer(SMALL, s, each * rounds(small * s, exact ? 0.6 : 0.34, exact ? 0.84 : 0.48));
+      offer(LARGE, s, each * rounds(large * s, exact ? 1.2 : 0.73, exact ? 1.87 : 1.05));
+      offer(SMALL, s, each * rounds(small * s, exact ? 0.5 : 0.3, exact ? 0.75 : 0.54));
     }
   }
   Plan& p = best.plan;
