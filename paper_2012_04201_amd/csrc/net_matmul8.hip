@@ -301,7 +301,7 @@ __global__ __launch_bounds__(64 * W) void k_mm_rows(const MatArgs whole) {
 // themselves (g.direct); a last part of a block, and rows at other addresses, through registers.
 // What bounds it, with two workgroups of 128 x 128 a CU: for float32 output 8192^3 takes 927 us (1.19 PFLOP/s, the library's bfloat16
 // product of that size 1.21); each matrix instruction has two conversions beside it, which run under it, and the vector instructions that
-// are left cost the most (scales decoded in every block: 1070 us).  For bfloat16 output the instructions fill a third of the cycles: a
+// are left cost the most (scales decoded in every block: 1070 us); the matrix units are busy in 54 % of the cycles, at 2.2 GHz.  For bfloat16 output the instructions fill a third of the cycles: a
 // block's way to LDS, which one workgroup waits for while the other multiplies, is as long as its products.
 // ---------------------------------------------------------------------------
 __device__ inline int mix(int row) { return (row & 7) ^ (row >> 3 & 1); }
@@ -606,7 +606,7 @@ __global__ __launch_bounds__(256, 2) void k_mm_small(const MatArgs whole, int ti
 // Waves 4 to 7 are a part behind, so that of the two waves of a SIMD one multiplies while the other loads.  Loads return in order: the
 // wait for some rows is a count of the younger loads.  It is made a quarter before the rows are read, and rows are asked for a
 // quarter after all waves have read what was in their place, as the other half of the waves needs.
-// What bounds it: 8192^3 takes 420 to 440 us (2.5 to 2.6 PFLOP/s; 360 us on zeros): the instructions fill 63 % of the cycles, at 1.92 GHz, which is the
+// What bounds it: 8192^3 takes 420 to 440 us (2.5 to 2.6 PFLOP/s; 360 us on zeros): the instructions fill 62 % of the cycles, at 1.9 to 2.0 GHz, which is the
 // power limit's doing; the barriers and the unequal parts are the rest.  Plain double buffering with one barrier a block: 474 us.  By quarters
 // without the shift of half the waves: 466.  With 32 x 32 x 64 instructions: 478, at a lower clock.
 // ---------------------------------------------------------------------------

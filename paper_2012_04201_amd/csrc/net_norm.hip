@@ -41,7 +41,7 @@ struct NormArgs {
 };
 
 // One pass: a row is read once, kept in registers over the reduction and written once.  Bound by those bytes: 16384 x 8192 in bfloat16 with
-// residual and sum takes 189 us (5.7 TB/s), 20000 x 1024 31 us (5.2 TB/s); one row of 4096 3.0 us, a launch.
+// residual and sum takes 189 us (5.7 TB/s), 20000 x 1024 31 us (5.2 TB/s); one row of 1024 3.0 us, a launch.
 // WHOLE: the width is a multiple of eight.
 template <typename E, int T, int NV, bool WHOLE>
 __global__ __launch_bounds__(T == 64 ? 256 : T) void k_rms_norm(const NormArgs a) {
