@@ -50,6 +50,16 @@ def test_codes_and_scales(net, rows, cols, dtype, tile, gated):
 
 
 @pytest.mark.parametrize("tile", [1, 128])
+def test_many_tiles(net, tile):
+    """As many as give a thread eight rows."""
+    x, gate = data(2600, 2499, torch.bfloat16)
+    q, qt = net.quantize(x.cuda(), tile, gate=gate.cuda(), want_cols=True)
+    want = torch.where(gate > 0, x.double(), 0.0).numpy()
+    same(q, want, tile)
+    same(qt, want.T, tile)
+
+
+@pytest.mark.parametrize("tile", [1, 128])
 def test_every_size_of_value(net, tile):
     """Ties, subnormal codes, powers of two at the scales' edges, zeros, values far below their block's largest, and what is not finite."""
     rows, cols = 40, 256
