@@ -9,6 +9,7 @@ Argument marshalling only, as in `binding`: every value is computed in the HIP k
 the stream.  Inputs are on the GPU; calls work on the current device's current stream, or on `stream`, and do not wait.
 """
 import ctypes as C
+import functools
 from collections import namedtuple
 
 import numpy as np
@@ -32,6 +33,8 @@ State8 = namedtuple("State8", "m m_scales v v_scales")
 
 _P, _I64, _I32, _F, _U64, _SZ = C.c_void_p, C.c_int64, C.c_int32, C.c_float, C.c_uint64, C.c_size_t
 _DTYPES = {torch.float32: F32, torch.bfloat16: BF16}
+_E4M3, _E8M0, _FLOAT = torch.float8_e4m3fn, torch.float8_e8m0fnu, torch.float32
+_new = torch.empty_strided
 
 
 class Tensor(C.Structure):
@@ -74,21 +77,22 @@ def _stream(stream, t):
 def _room(stream, shape, stride, dtype, device):
     """A tensor for an output: under the stream that will use it."""
     if stream is None:
-        return torch.empty_strided(shape, stride, dtype=dtype, device=device)
+        return _new(shape, stride, dtype=dtype, device=device)
     with torch.cuda.stream(stream):
-        return torch.empty_strided(shape, stride, dtype=dtype, device=device)
+        return _new(shape, stride, dtype=dtype, device=device)
 
 
 def _matrix(t, name, like=None):
     """A [rows, cols] tensor on the GPU whose rows are dense; of another's type, shape and device."""
-    if t.dim() != 2 or (t.stride(1) != 1 and t.shape[1] > 1):
+    shape = t.shape
+    if len(shape) != 2 or (t.stride(1) != 1 and shape[1] > 1):
         raise ValueError("%s must be a [rows, cols] tensor with dense rows" % name)
     if like is None:
         if t.dtype not in _DTYPES:
             raise ValueError("%s must be float32 or bfloat16" % name)
         if not t.is_cuda:
             raise ValueError("%s must be on the GPU" % name)
-    elif t.dtype is not like.dtype or t.shape != like.shape or t.device != like.device:
+    elif t.dtype is not like.dtype or shape != like.shape or t.get_device() != like.get_device():
         raise ValueError("%s must be %s %s on %s" % (name, like.dtype, tuple(like.shape), like.device))
 
 
@@ -97,33 +101,47 @@ def _row(t):
     return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
 
 
-def _vector(t, name, n, device):
-    if t.dtype is not torch.float32 or t.dim() != 1 or t.shape[0] != n or not t.is_contiguous() or t.device != device or not t.is_cuda:
+def _vector(t, name, n, like):
+    if t.dtype is not _FLOAT or t.shape != (n,) or not t.is_contiguous() or t.get_device() != like.get_device():
         raise ValueError("%s must be a dense float32 [%d] tensor on the same GPU" % (name, n))
 
 
 def empty_blocks8(rows, cols, tile=1, device="cuda", stream=None):
     """Room for an 8-bit matrix: rows at multiples of 128 bytes, their scales at multiples of 4."""
-    kb, sr = -(-cols // BLOCK), -(-rows // tile)
-    full, sfull = kb * BLOCK, -(-kb // 4) * 4
-    v = _room(stream, (rows, full), (full, 1), torch.float8_e4m3fn, device)
-    s = _room(stream, (sr, sfull), (sfull, 1), torch.float8_e8m0fnu, device)
-    return Blocks8(v if full == cols else v[:, :cols], s if sfull == kb else s[:, :kb], tile)
+    kb = (cols + 127) >> 7
+    v = _room(stream, (rows, cols), (kb * BLOCK, 1), _E4M3, device)
+    s = _room(stream, (rows if tile == 1 else (rows + 127) >> 7, kb), ((kb + 3) & ~3, 1), _E8M0, device)
+    return Blocks8(v, s, tile)
 
 
 def _check_blocks(b, name):
     v, s, tile = b
     if tile != 1 and tile != BLOCK:
         raise ValueError("%s: tile must be 1 or 128" % name)
-    if v.dim() != 2 or v.dtype is not torch.float8_e4m3fn or (v.stride(1) != 1 and v.shape[1] > 1):
+    shape = v.shape
+    if len(shape) != 2 or v.dtype is not _E4M3 or (v.stride(1) != 1 and shape[1] > 1):
         raise ValueError("%s: values must be float8_e4m3fn [rows, cols] with dense rows" % name)
-    rows, cols = v.shape
-    want = (-(-rows // tile), -(-cols // BLOCK))
-    if s.dtype is not torch.float8_e8m0fnu or s.shape != want or (s.stride(1) != 1 and want[1] > 1):
+    rows, cols = shape
+    want = (rows if tile == 1 else (rows + 127) >> 7, (cols + 127) >> 7)
+    if s.dtype is not _E8M0 or s.shape != want or (s.stride(1) != 1 and want[1] > 1):
         raise ValueError("%s: scales must be float8_e8m0fnu %s with dense rows" % (name, want))
-    if not v.is_cuda or s.device != v.device:
+    if not v.is_cuda or s.get_device() != v.get_device():
         raise ValueError("%s must be on the GPU" % name)
     return rows, cols
+
+
+@functools.lru_cache(4096)
+def _product_room(m, n, k):
+    need = _SZ(0)
+    _check(lib().bbo_net_matmul8_workspace(m, n, k, C.byref(need)))
+    return need.value
+
+
+@functools.lru_cache(4096)
+def _grad_room(rows, width):
+    need = _SZ(0)
+    _check(lib().bbo_net_rms_norm_grad_workspace(rows, width, C.byref(need)))
+    return max(need.value, 256)
 
 
 def rms_norm(x, weight=None, residual=None, eps=1e-6, want_y=True, want_rstd=False, want_8bit=False, stream=None):
@@ -142,7 +160,7 @@ def rms_norm(x, weight=None, residual=None, eps=1e-6, want_y=True, want_rstd=Fal
         h = _room(stream, (rows, width), (width, 1), dtype, device)
         ph = h.data_ptr()
     if weight is not None:
-        _vector(weight, "weight", width, device)
+        _vector(weight, "weight", width, x)
         pw = weight.data_ptr()
     if want_y:
         y = _room(stream, (rows, width), (width, 1), dtype, device)
@@ -166,13 +184,13 @@ def rms_norm_grad(dy, h, rstd, weight=None, dsum=None, want_dweight=True, worksp
     rows, width = h.shape
     dtype, device = h.dtype, h.device
     _matrix(dy, "dy", h)
-    _vector(rstd, "rstd", rows, device)
+    _vector(rstd, "rstd", rows, h)
     pd = pw = pg = ws = room = d_stride = 0
     if dsum is not None:
         _matrix(dsum, "dsum", h)
         pd, d_stride = dsum.data_ptr(), _row(dsum)
     if weight is not None:
-        _vector(weight, "weight", width, device)
+        _vector(weight, "weight", width, h)
         pw = weight.data_ptr()
     dx, dw = _room(stream, (rows, width), (width, 1), dtype, device), None
     L = _net or lib()
@@ -180,9 +198,7 @@ def rms_norm_grad(dy, h, rstd, weight=None, dsum=None, want_dweight=True, worksp
         dw = _room(stream, (width,), (1,), torch.float32, device)
         pg = dw.data_ptr()
         if workspace is None:
-            need = _SZ(0)
-            _check(L.bbo_net_rms_norm_grad_workspace(rows, width, C.byref(need)))
-            workspace = _room(stream, (max(need.value, 256),), (1,), torch.uint8, device)
+            workspace = _room(stream, (_grad_room(rows, width),), (1,), torch.uint8, device)
         elif workspace.device != device or not workspace.is_contiguous():
             raise ValueError("workspace must be dense and on the same GPU")
         ws, room = workspace.data_ptr(), workspace.numel() * workspace.element_size()
@@ -216,7 +232,8 @@ def quantize(x, tile=1, gate=None, want_rows=True, want_cols=False, stream=None)
 def matmul8(a, b, dtype=torch.bfloat16, out=None, accumulate=False, workspace=None, stream=None):
     """a b^T of two Blocks8 [m, k] and [n, k] -> [m, n] in float32 or bfloat16; accumulate adds to `out`."""
     (m, k), (n, kb) = _check_blocks(a, "a"), _check_blocks(b, "b")
-    av, bv, device = a.values, b.values, a.values.device
+    av, bv = a.values, b.values
+    on, device = av.get_device(), av.device
     if kb != k:
         raise ValueError("a and b must have rows of the same length")
     if out is None:
@@ -229,14 +246,13 @@ def matmul8(a, b, dtype=torch.bfloat16, out=None, accumulate=False, workspace=No
         _matrix(out, "out")
         if out.shape != (m, n):
             raise ValueError("out must have the shape %s" % ((m, n),))
-    if bv.device != device or out.device != device:
+    if bv.get_device() != on or out.get_device() != on:
         raise ValueError("all tensors must be on the same GPU")
     L, ws, room = _net or lib(), 0, 0
     if workspace is None:
-        need = _SZ(0)
-        _check(L.bbo_net_matmul8_workspace(m, n, k, C.byref(need)))
-        if need.value:
-            workspace = _room(stream, (need.value,), (1,), torch.uint8, device)
+        need = _product_room(m, n, k)
+        if need:
+            workspace = _room(stream, (need,), (1,), torch.uint8, device)
     elif workspace.device != device or not workspace.is_contiguous():
         raise ValueError("workspace must be dense and on the same GPU")
     if workspace is not None:
@@ -323,7 +339,7 @@ class AdamW:
         self._rates[:, 0], self._rates[:, 1] = self.lr, self.weight_decay
         scale = 0
         if grad_scale is not None:
-            _vector(grad_scale.view(-1), "grad_scale", 1, device)
+            _vector(grad_scale.view(-1), "grad_scale", 1, params[0])
             scale = grad_scale.data_ptr()
         _check((_net or lib()).bbo_net_adamw(self._table, n, _DTYPES[params[0].dtype], _DTYPES[dtype], self.eight, self.betas[0], self.betas[1], self.eps,
                                              self.steps + 1, self.seed, scale, _stream(stream, params[0])))

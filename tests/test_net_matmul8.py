@@ -18,14 +18,13 @@ def net():
 def matrix(net, rows, cols, tile, seed, pad=True, scales=(100, 140)):
     """Random codes and scales, with NaN where nothing is to be read."""
     g = torch.Generator().manual_seed(seed)
-    b = net.empty_blocks8(rows, cols, tile)
-    if not pad:  # dense rows, at odd addresses for odd lengths
-        kb = -(-cols // 128)
+    kb, sr = -(-cols // 128), -(-rows // tile)
+    if pad:
+        b = net.Blocks8(torch.full((rows, kb * 128), 0x7f, dtype=torch.uint8).cuda().view(torch.float8_e4m3fn)[:, :cols],
+                        torch.full((sr, -(-kb // 4) * 4), 255, dtype=torch.uint8).cuda().view(torch.float8_e8m0fnu)[:, :kb], tile)
+    else:  # dense rows, at odd addresses for odd lengths
         b = net.Blocks8(torch.empty(rows, cols, dtype=torch.uint8).cuda().view(torch.float8_e4m3fn),
-                        torch.empty(-(-rows // tile), kb, dtype=torch.uint8).cuda().view(torch.float8_e8m0fnu), tile)
-    elif rows:
-        b.values.view(torch.uint8).as_strided((rows, b.values.stride(0)), (b.values.stride(0), 1)).fill_(0x7f)
-        b.scales.view(torch.uint8).as_strided((b.scales.shape[0], b.scales.stride(0)), (b.scales.stride(0), 1)).fill_(255)
+                        torch.empty(sr, kb, dtype=torch.uint8).cuda().view(torch.float8_e8m0fnu), tile)
     codes = torch.randint(0, 127, (rows, cols), generator=g) | (torch.randint(0, 2, (rows, cols), generator=g) << 7)
     b.values.view(torch.uint8).copy_(codes.to(torch.uint8))
     b.scales.view(torch.uint8).copy_(torch.randint(*scales, tuple(b.scales.shape), generator=g).to(torch.uint8))
