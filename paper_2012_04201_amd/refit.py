@@ -47,16 +47,35 @@ class WideNetwork:
         pairs = [net.quantize(w, tile=128, want_cols=True) for w in self.w]
         self.w8, self.w8t = [p[0] for p in pairs], [p[1] for p in pairs]
 
-    def predict(self, x):
-        """Logits (or values) float32 [rows, outputs]; the norm's output goes straight into 8 bits."""
-        h = net.matmul8(net.quantize(x)[0], self.w8[0])
-        n = net.rms_norm(h, self.norms[0], want_y=False, want_8bit=True)
+    def predict(self, x, weights=None):
+        """Logits (or values) float32 [rows, outputs]; the norm's output goes straight into 8 bits.  weights: of server()."""
+        w8, norms = weights or (self.w8, self.norms)
+        h = net.matmul8(net.quantize(x)[0], w8[0])
+        n = net.rms_norm(h, norms[0], want_y=False, want_8bit=True)
         for i in range(self.blocks):
-            u = net.matmul8(n.y8, self.w8[2 * i + 1])
-            o = net.matmul8(net.quantize(u, gate=u)[0], self.w8[2 * i + 2])
-            n = net.rms_norm(o, self.norms[i + 1], residual=h, want_y=False, want_8bit=True)
+            u = net.matmul8(n.y8, w8[2 * i + 1])
+            o = net.matmul8(net.quantize(u, gate=u)[0], w8[2 * i + 2])
+            n = net.rms_norm(o, norms[i + 1], residual=h, want_y=False, want_8bit=True)
             h = n.sum
-        return net.matmul8(n.y8, self.w8[-1], torch.float32)
+        return net.matmul8(n.y8, w8[-1], torch.float32)
+
+    def server(self, rows=1):
+        """predict() for `rows` rows as one launch of a captured graph: a function of x whose result the next call overwrites.
+
+        It answers with the weights of now, whatever step() makes of them."""
+        weights = self.w8, [w.clone() for w in self.norms]  # (step() makes new 8-bit copies, and changes the norms in place)
+        x = torch.zeros(rows, self.w[0].shape[1], dtype=BF16, device=self.w[0].device)
+        self.predict(x, weights)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            out = self.predict(x, weights)
+
+        def serve(rows_in, weights=weights):  # (which keeps what the graph reads)
+            x.copy_(rows_in)
+            graph.replay()
+            return out
+        return serve
 
     def gradients(self, x, y):
         """(loss, gradients of w and norms in their order) of a batch: cross entropy, or half the squared error."""
@@ -130,12 +149,12 @@ def refit(cfg, width=1024, hidden=2048, blocks=2, epochs=20, batch=512, lr=1e-3,
     seconds = time.perf_counter() - start
     p = model.predict(Xv)
     score = (p.argmax(1) == yv).float().mean() if classes else -(p[:, 0] - yv).square().mean()
-    row = Xv[:1].contiguous()
-    model.predict(row)
+    row, serve = Xv[:1].contiguous(), model.server(1)
+    serve(row)
     torch.cuda.synchronize()
     start = time.perf_counter()
     for _ in range(20):
-        model.predict(row)
+        serve(row)
     torch.cuda.synchronize()
     return model, {"rows": len(yt), "steps": steps, "loss": losses, "score": float(score), "ms_per_step": 1e3 * seconds / max(steps, 1),
                    "us_per_served_row": (time.perf_counter() - start) / 20 * 1e6}

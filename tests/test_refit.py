@@ -60,6 +60,23 @@ def test_it_learns_and_serves(refit):
     assert r2["loss"] == r["loss"][:2]  # the same bits from the same seed
 
 
+@pytest.mark.parametrize("rows", [1, 5, 64])
+def test_served_from_a_graph(refit, rows):
+    g = torch.Generator().manual_seed(6)
+    model = refit.WideNetwork(30, 4, 256, 300, 2, seed=5)
+    serve = model.server(rows)
+    for i in range(4):
+        x = torch.randn(rows, 30, generator=g).bfloat16().cuda()
+        got = serve(x).clone()
+        torch.cuda.synchronize()
+        assert torch.equal(got, model.predict(x))
+        torch.cuda.synchronize()
+    before = serve(x).clone()
+    model.step(torch.randn(100, 30, generator=g).bfloat16().cuda(), torch.randint(0, 4, (100,), generator=g).cuda())
+    assert torch.equal(serve(x).clone(), before)  # the weights of its making
+    assert torch.equal(model.server(rows)(x).clone(), model.predict(x)) and not torch.equal(model.predict(x), before)
+
+
 def test_it_fits_values(refit):
     g = np.random.default_rng(4)
     X = g.normal(size=(600, 13)).astype(np.float32)
