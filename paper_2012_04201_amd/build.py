@@ -1,4 +1,4 @@
-"""Builds libbbo_mlp.so (HIP, gfx950) in-tree with hipcc, the kernel families side by side, and the packer of suggestions."""
+"""Builds libbbo_mlp.so (HIP, gfx950) in-tree with hipcc, the kernel families side by side, the packer of suggestions and the network operators' torch side."""
 import os
 import subprocess
 import sysconfig
@@ -35,6 +35,12 @@ def build_lib(verbose=False):
         print(err)
     _run(["gcc", "-O2", "-shared", "-fPIC", "-Wall", "-I" + sysconfig.get_paths()["include"],
           os.path.join(CSRC, "pack_hparams.c"), "-o", os.path.join(HERE, "_pack.so")])
+    import torch
+    base = os.path.dirname(torch.__file__)
+    _run(["g++", "-O2", "-std=c++17", "-shared", "-fPIC", "-Wall", "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch._C._GLIBCXX_USE_CXX11_ABI,
+          "-isystem" + os.path.join(base, "include"), "-isystem" + os.path.join(base, "include", "torch", "csrc", "api", "include"),
+          "-I" + sysconfig.get_paths()["include"], os.path.join(CSRC, "net_torch.cpp"), "-o", os.path.join(HERE, "_net.so"),
+          "-L" + os.path.join(base, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10"])
     return LIB
 
 

@@ -1,0 +1,311 @@
+// The network operators on torch tensors: checks of what the C ABI cannot see, outputs, and the call.  A call from Python spends less
+// here than its kernel's launch takes (a row through the norm, three outputs: 10 us by ctypes and torch's Python functions).
+#include <Python.h>
+
+#include <ATen/ops/empty_strided.h>
+#include <torch/csrc/Exceptions.h>
+#include <torch/csrc/autograd/python_variable.h>
+
+#include <algorithm>
+#include <string>
+
+#include "../../include/bbo_net.h"
+
+namespace {
+
+struct Refused {
+  std::string why;
+};
+[[noreturn]] void refuse(const std::string& why) { throw Refused{why}; }
+
+// The library's functions, by the addresses that bind() was given, and what raises an error for a code that is not BBO_OK.
+decltype(&bbo_net_rms_norm) f_norm;
+decltype(&bbo_net_rms_norm_grad_workspace) f_grad_room;
+decltype(&bbo_net_rms_norm_grad) f_grad;
+decltype(&bbo_net_quantize) f_quantize;
+decltype(&bbo_net_matmul8_workspace) f_product_room;
+decltype(&bbo_net_matmul8) f_product;
+decltype(&bbo_net_adamw) f_adamw;
+PyObject* g_check;
+
+bool failed(int code) {  // with the Python error set
+  if (code == BBO_OK) return false;
+  PyObject* r = PyObject_CallFunction(g_check, "i", code);
+  Py_XDECREF(r);
+  return true;
+}
+
+const at::Tensor& tensor(PyObject* o, const char* name) {
+  if (!THPVariable_Check(o)) refuse(std::string(name) + " must be a tensor");
+  return THPVariable_Unpack(o);
+}
+bool given(PyObject* o) { return o != Py_None; }
+void* stream_of(PyObject* o) { return PyLong_AsVoidPtr(o); }
+int code_of(const at::Tensor& t) { return t.scalar_type() == at::kFloat ? BBO_F32 : BBO_BF16; }
+bool is_float(const at::Tensor& t) { return t.scalar_type() == at::kFloat || t.scalar_type() == at::kBFloat16; }
+bool dense_rows(const at::Tensor& t) { return t.dim() == 2 && (t.size(1) <= 1 || t.stride(1) == 1); }
+// The distance of a matrix's rows: a single row's stride says nothing.
+int64_t row(const at::Tensor& t) { return t.size(0) > 1 ? t.stride(0) : std::max(t.stride(0), t.size(1)); }
+
+const at::Tensor& matrix(PyObject* o, const char* name) {
+  const at::Tensor& t = tensor(o, name);
+  if (!dense_rows(t)) refuse(std::string(name) + " must be a [rows, cols] tensor with dense rows");
+  if (!is_float(t)) refuse(std::string(name) + " must be float32 or bfloat16");
+  if (!t.is_cuda()) refuse(std::string(name) + " must be on the GPU");
+  return t;
+}
+const at::Tensor& matrix_like(PyObject* o, const char* name, const at::Tensor& like) {
+  const at::Tensor& t = tensor(o, name);
+  if (!dense_rows(t)) refuse(std::string(name) + " must be a [rows, cols] tensor with dense rows");
+  if (t.scalar_type() != like.scalar_type() || t.sizes() != like.sizes() || t.device() != like.device())
+    refuse(std::string(name) + " must have the type, shape and GPU of the others");
+  return t;
+}
+const float* vector(PyObject* o, const char* name, int64_t n, const at::Tensor& like) {
+  const at::Tensor& t = tensor(o, name);
+  if (t.scalar_type() != at::kFloat || t.dim() != 1 || t.size(0) != n || !t.is_contiguous() || t.device() != like.device())
+    refuse(std::string(name) + " must be a dense float32 [" + std::to_string(n) + "] tensor on the same GPU");
+  return (const float*)t.data_ptr();
+}
+at::Tensor room(const at::Tensor& like, int64_t rows, int64_t cols, int64_t stride, at::ScalarType type) {
+  return at::empty_strided({rows, cols}, {stride, 1}, like.options().dtype(type));
+}
+at::Tensor room1(const at::Tensor& like, int64_t n, at::ScalarType type) { return at::empty_strided({n}, {1}, like.options().dtype(type)); }
+
+struct Blocks {
+  at::Tensor values, scales;
+};
+int64_t blocks_of(int64_t n) { return (n + 127) >> 7; }
+// Rows at multiples of 128 bytes, their scales at multiples of 4.
+Blocks blocks_room(const at::Tensor& like, int64_t rows, int64_t cols, int tile) {
+  const int64_t kb = blocks_of(cols);
+  return {room(like, rows, cols, kb * 128, at::kFloat8_e4m3fn),
+          room(like, tile == 1 ? rows : blocks_of(rows), kb, (kb + 3) & ~3ll, at::kFloat8_e8m0fnu)};
+}
+int tile_of(PyObject* o, const char* name) {
+  const long tile = PyLong_Check(o) ? PyLong_AsLong(o) : 0;
+  if (tile != 1 && tile != 128) refuse(std::string(name) + "tile must be 1 or 128");
+  return (int)tile;
+}
+struct Operand {
+  const at::Tensor &values, &scales;
+  int tile;
+};
+Operand operand(PyObject* values, PyObject* scales, PyObject* tile, const char* name) {
+  const std::string n = name;
+  const Operand b{tensor(values, name), tensor(scales, name), tile_of(tile, (n + ": ").c_str())};
+  if (!dense_rows(b.values) || b.values.scalar_type() != at::kFloat8_e4m3fn)
+    refuse(n + ": values must be float8_e4m3fn [rows, cols] with dense rows");
+  if (!dense_rows(b.scales) || b.scales.scalar_type() != at::kFloat8_e8m0fnu || b.scales.size(1) != blocks_of(b.values.size(1)) ||
+      b.scales.size(0) != (b.tile == 1 ? b.values.size(0) : blocks_of(b.values.size(0))))
+    refuse(n + ": scales must be float8_e8m0fnu, one for each block, with dense rows");
+  if (!b.values.is_cuda() || b.scales.device() != b.values.device()) refuse(n + " must be on the GPU");
+  return b;
+}
+// A caller's workspace, or one of `need` bytes.
+at::Tensor workspace_of(PyObject* o, size_t need, const at::Tensor& like) {
+  if (!given(o)) return need ? room1(like, (int64_t)need, at::kByte) : at::Tensor();
+  const at::Tensor& t = tensor(o, "workspace");
+  if (t.device() != like.device() || !t.is_contiguous()) refuse("workspace must be dense and on the same GPU");
+  return t;
+}
+
+PyObject* wrapped(at::Tensor t) {
+  if (t.defined()) return THPVariable_Wrap(std::move(t));
+  Py_RETURN_NONE;
+}
+// A tuple of tensors, None for those that are not there.
+template <typename... T>
+PyObject* tuple(T... t) {
+  PyObject* r = PyTuple_New(sizeof...(T));
+  if (!r) return nullptr;
+  Py_ssize_t i = 0;
+  bool ok = true;
+  auto put = [&](at::Tensor x) {
+    PyObject* o = wrapped(std::move(x));
+    ok &= o != nullptr;
+    PyTuple_SET_ITEM(r, i++, o);
+  };
+  (put(std::move(t)), ...);
+  if (!ok) {
+    Py_DECREF(r);
+    return nullptr;
+  }
+  return r;
+}
+
+// x, weight, residual, eps, want_y, want_rstd, want_8bit, stream -> y, sum, rstd, values, scales
+PyObject* norm(PyObject* const* a) {
+  const at::Tensor& x = matrix(a[0], "x");
+  const int64_t rows = x.size(0), width = x.size(1);
+  const float* w = given(a[1]) ? vector(a[1], "weight", width, x) : nullptr;
+  const at::Tensor* residual = given(a[2]) ? &matrix_like(a[2], "residual", x) : nullptr;
+  const double eps = PyFloat_AsDouble(a[3]);
+  if (PyErr_Occurred()) return nullptr;
+  at::Tensor sum, y, rstd;
+  Blocks q;
+  if (residual) sum = room(x, rows, width, width, x.scalar_type());
+  if (PyObject_IsTrue(a[4])) y = room(x, rows, width, width, x.scalar_type());
+  if (PyObject_IsTrue(a[5])) rstd = room1(x, rows, at::kFloat);
+  const bool eight = PyObject_IsTrue(a[6]);
+  if (eight) q = blocks_room(x, rows, width, 1);
+  if (failed(f_norm(x.data_ptr(), row(x), residual ? residual->data_ptr() : nullptr, residual ? row(*residual) : 0, w, rows, width,
+                    (float)eps, code_of(x), residual ? sum.data_ptr() : nullptr, width, y.defined() ? y.data_ptr() : nullptr, width,
+                    rstd.defined() ? (float*)rstd.data_ptr() : nullptr, eight ? q.values.data_ptr() : nullptr, eight ? row(q.values) : 0,
+                    eight ? q.scales.data_ptr() : nullptr, eight ? row(q.scales) : 0, stream_of(a[7]))))
+    return nullptr;
+  return tuple(std::move(y), std::move(sum), std::move(rstd), std::move(q.values), std::move(q.scales));
+}
+
+// dy, h, rstd, weight, dsum, want_dweight, workspace, stream -> dx, dweight
+PyObject* norm_grad(PyObject* const* a) {
+  const at::Tensor& h = matrix(a[1], "h");
+  const int64_t rows = h.size(0), width = h.size(1);
+  const at::Tensor& dy = matrix_like(a[0], "dy", h);
+  const float* rstd = vector(a[2], "rstd", rows, h);
+  const float* w = given(a[3]) ? vector(a[3], "weight", width, h) : nullptr;
+  const at::Tensor* dsum = given(a[4]) ? &matrix_like(a[4], "dsum", h) : nullptr;
+  at::Tensor dx = room(h, rows, width, width, h.scalar_type()), dw, ws;
+  if (PyObject_IsTrue(a[5])) {
+    dw = room1(h, width, at::kFloat);
+    size_t need = 0;
+    if (!given(a[6]) && failed(f_grad_room(rows, width, &need))) return nullptr;
+    ws = workspace_of(a[6], std::max<size_t>(need, 256), h);
+  }
+  if (failed(f_grad(dy.data_ptr(), row(dy), dsum ? dsum->data_ptr() : nullptr, dsum ? row(*dsum) : 0, h.data_ptr(), row(h), rstd, w, rows,
+                    width, code_of(h), dx.data_ptr(), width, dw.defined() ? (float*)dw.data_ptr() : nullptr,
+                    ws.defined() ? ws.data_ptr() : nullptr, ws.defined() ? ws.nbytes() : 0, stream_of(a[7]))))
+    return nullptr;
+  return tuple(std::move(dx), std::move(dw));
+}
+
+// x, tile, gate, want_rows, want_cols, stream -> values, scales, values and scales of the transpose
+PyObject* quantize(PyObject* const* a) {
+  const at::Tensor& x = matrix(a[0], "x");
+  const int64_t rows = x.size(0), cols = x.size(1);
+  const at::Tensor* gate = given(a[2]) ? &matrix_like(a[2], "gate", x) : nullptr;
+  const int tile = tile_of(a[1], "");
+  const bool own = PyObject_IsTrue(a[3]), turned = PyObject_IsTrue(a[4]);
+  Blocks q, t;
+  if (own) q = blocks_room(x, rows, cols, tile);
+  if (turned) t = blocks_room(x, cols, rows, tile);
+  if (failed(f_quantize(x.data_ptr(), row(x), gate ? gate->data_ptr() : nullptr, gate ? row(*gate) : 0, rows, cols, code_of(x), tile,
+                        own ? q.values.data_ptr() : nullptr, own ? row(q.values) : 0, own ? q.scales.data_ptr() : nullptr,
+                        own ? row(q.scales) : 0, turned ? t.values.data_ptr() : nullptr, turned ? row(t.values) : 0,
+                        turned ? t.scales.data_ptr() : nullptr, turned ? row(t.scales) : 0, stream_of(a[5]))))
+    return nullptr;
+  return tuple(std::move(q.values), std::move(q.scales), std::move(t.values), std::move(t.scales));
+}
+
+// a's values, scales, tile, b's, whether to float32, out, accumulate, workspace, stream -> the output
+PyObject* product(PyObject* const* p) {
+  const Operand a = operand(p[0], p[1], p[2], "a"), b = operand(p[3], p[4], p[5], "b");
+  const int64_t m = a.values.size(0), n = b.values.size(0), k = a.values.size(1);
+  if (b.values.size(1) != k) refuse("a and b must have rows of the same length");
+  const bool add = PyObject_IsTrue(p[8]);
+  if (!given(p[7]) && add) refuse("accumulate needs an output to add to");
+  if (given(p[7])) {
+    const at::Tensor& out = matrix(p[7], "out");
+    if (out.size(0) != m || out.size(1) != n) refuse("out must have the shape (" + std::to_string(m) + ", " + std::to_string(n) + ")");
+    if (out.device() != a.values.device()) refuse("all tensors must be on the same GPU");
+  }
+  if (b.values.device() != a.values.device()) refuse("all tensors must be on the same GPU");
+  const at::Tensor out = given(p[7]) ? THPVariable_Unpack(p[7]) : room(a.values, m, n, n, PyObject_IsTrue(p[6]) ? at::kFloat : at::kBFloat16);
+  size_t need = 0;
+  if (!given(p[9]) && failed(f_product_room(m, n, k, &need))) return nullptr;
+  const at::Tensor ws = workspace_of(p[9], need, a.values);
+  if (failed(f_product(a.values.data_ptr(), row(a.values), a.scales.data_ptr(), row(a.scales), a.tile, b.values.data_ptr(), row(b.values),
+                       b.scales.data_ptr(), row(b.scales), b.tile, m, n, k, out.data_ptr(), row(out), code_of(out), add,
+                       ws.defined() ? ws.data_ptr() : nullptr, ws.defined() ? ws.nbytes() : 0, stream_of(p[10]))))
+    return nullptr;
+  if (given(p[7])) {
+    Py_INCREF(p[7]);
+    return p[7];
+  }
+  return wrapped(out);
+}
+
+// address of the records, parameters, gradients, learning rates, decays, whether in 8 bits, beta1, beta2, eps, step, seed, grad_scale, stream
+PyObject* adamw(PyObject* const* a) {
+  auto* table = (bbo_net_tensor*)PyLong_AsVoidPtr(a[0]);
+  PyObject *ps = a[1], *gs = a[2], *lr = a[3], *wd = a[4];
+  if (!PyList_Check(ps) || !PyList_Check(gs) || !PyList_Check(lr) || !PyList_Check(wd)) refuse("parameters, gradients and rates must be lists");
+  const Py_ssize_t n = PyList_GET_SIZE(ps);
+  if (PyList_GET_SIZE(gs) != n) refuse("one gradient per parameter");
+  if (PyList_GET_SIZE(lr) != n || PyList_GET_SIZE(wd) != n) refuse("one learning rate and decay per parameter");
+  if (n == 0) Py_RETURN_NONE;
+  const at::Tensor& first = tensor(PyList_GET_ITEM(gs, 0), "gradient");
+  const at::Tensor& p0 = tensor(PyList_GET_ITEM(ps, 0), "parameter");
+  if (!is_float(first)) refuse("gradients must be float32 or bfloat16");
+  for (Py_ssize_t i = 0; i < n; i++) {
+    const at::Tensor& g = tensor(PyList_GET_ITEM(gs, i), "gradient");
+    const at::Tensor& p = tensor(PyList_GET_ITEM(ps, i), "parameter");
+    if (g.scalar_type() != first.scalar_type() || g.numel() != table[i].n || !g.is_contiguous() || g.device() != p0.device())
+      refuse("gradients must be dense, of the parameters' sizes, of one type and on their GPU");
+    if (p.scalar_type() != p0.scalar_type() || p.numel() != table[i].n || !p.is_contiguous() || p.device() != p0.device())
+      refuse("parameters must stay as they were");
+    table[i].p = p.data_ptr();
+    table[i].g = g.data_ptr();
+    table[i].lr = (float)PyFloat_AsDouble(PyList_GET_ITEM(lr, i));
+    table[i].weight_decay = (float)PyFloat_AsDouble(PyList_GET_ITEM(wd, i));
+  }
+  const double b1 = PyFloat_AsDouble(a[6]), b2 = PyFloat_AsDouble(a[7]), eps = PyFloat_AsDouble(a[8]);
+  const long long step = PyLong_AsLongLong(a[9]);
+  const unsigned long long seed = PyLong_AsUnsignedLongLongMask(a[10]);
+  if (PyErr_Occurred()) return nullptr;
+  const float* scale = nullptr;
+  if (given(a[11])) {
+    const at::Tensor& t = tensor(a[11], "grad_scale");
+    if (t.scalar_type() != at::kFloat || t.numel() != 1 || t.device() != p0.device()) refuse("grad_scale must be a float32 [1] tensor on the same GPU");
+    scale = (const float*)t.data_ptr();
+  }
+  if (failed(f_adamw(table, (int32_t)n, code_of(p0), code_of(first), PyObject_IsTrue(a[5]) ? BBO_NET_MOMENTS_8BIT : BBO_NET_MOMENTS_F32, b1, b2, eps,
+                     step, seed, scale, stream_of(a[12]))))
+    return nullptr;
+  Py_RETURN_NONE;
+}
+
+// what raises errors, addresses of the seven functions in the order above
+PyObject* bind(PyObject* const* a) {
+  Py_INCREF(a[0]);
+  Py_XDECREF(g_check);
+  g_check = a[0];
+  f_norm = (decltype(f_norm))PyLong_AsVoidPtr(a[1]);
+  f_grad_room = (decltype(f_grad_room))PyLong_AsVoidPtr(a[2]);
+  f_grad = (decltype(f_grad))PyLong_AsVoidPtr(a[3]);
+  f_quantize = (decltype(f_quantize))PyLong_AsVoidPtr(a[4]);
+  f_product_room = (decltype(f_product_room))PyLong_AsVoidPtr(a[5]);
+  f_product = (decltype(f_product))PyLong_AsVoidPtr(a[6]);
+  f_adamw = (decltype(f_adamw))PyLong_AsVoidPtr(a[7]);
+  if (PyErr_Occurred()) return nullptr;
+  Py_RETURN_NONE;
+}
+
+template <PyObject* (*F)(PyObject* const*), int ARGS>
+PyObject* entry(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  if (n != ARGS || (F != bind && !g_check)) {
+    PyErr_SetString(PyExc_TypeError, "wrong number of arguments, or not bound");
+    return nullptr;
+  }
+  try {
+    return F(args);
+  } catch (const Refused& r) {
+    PyErr_SetString(PyExc_ValueError, r.why.c_str());
+    return nullptr;
+  }
+  END_HANDLE_TH_ERRORS
+}
+
+PyMethodDef g_methods[] = {{"bind", (PyCFunction)(void*)entry<bind, 8>, METH_FASTCALL, nullptr},
+                           {"rms_norm", (PyCFunction)(void*)entry<norm, 8>, METH_FASTCALL, nullptr},
+                           {"rms_norm_grad", (PyCFunction)(void*)entry<norm_grad, 8>, METH_FASTCALL, nullptr},
+                           {"quantize", (PyCFunction)(void*)entry<quantize, 6>, METH_FASTCALL, nullptr},
+                           {"matmul8", (PyCFunction)(void*)entry<product, 11>, METH_FASTCALL, nullptr},
+                           {"adamw", (PyCFunction)(void*)entry<adamw, 13>, METH_FASTCALL, nullptr},
+                           {nullptr, nullptr, 0, nullptr}};
+PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_net", "The network operators on torch tensors.", -1, g_methods};
+
+}  // namespace
+
+PyMODINIT_FUNC PyInit__net() { return PyModule_Create(&g_module); }

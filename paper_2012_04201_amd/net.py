@@ -5,14 +5,13 @@
     y = net.matmul8(norm.y8, w8)                                      # y = norm(x + r) weight^T
     opt = net.AdamW(params, lr=1e-3, state="8bit"); opt.step(grads)
 
-Argument marshalling only, as in `binding`: every value is computed in the HIP kernels, PyTorch supplies device memory and
-the stream.  Inputs are on the GPU; calls work on the current device's current stream, or on `stream`, and do not wait.
+Every value is computed in the HIP kernels, PyTorch supplies device memory and the stream; arguments are checked and outputs made
+in the extension `_net` (csrc/net_torch.cpp).  Inputs are on the GPU; calls work on the current device's current stream, or on
+`stream`, and do not wait.
 """
 import ctypes as C
-import functools
 from collections import namedtuple
 
-import numpy as np
 import torch
 
 from . import binding
@@ -33,8 +32,6 @@ State8 = namedtuple("State8", "m m_scales v v_scales")
 
 _P, _I64, _I32, _F, _U64, _SZ = C.c_void_p, C.c_int64, C.c_int32, C.c_float, C.c_uint64, C.c_size_t
 _DTYPES = {torch.float32: F32, torch.bfloat16: BF16}
-_E4M3, _E8M0, _FLOAT = torch.float8_e4m3fn, torch.float8_e8m0fnu, torch.float32
-_new = torch.empty_strided
 
 
 class Tensor(C.Structure):
@@ -42,12 +39,13 @@ class Tensor(C.Structure):
                 ("lr", _F), ("weight_decay", _F)]
 
 
-_net = None
+_net = None  # the library, and the extension that calls it
+_ext = None
 
 
 def lib():
     """The shared library with these functions' argument types."""
-    global _net
+    global _net, _ext
     if _net is None:
         L = binding.lib()
         L.bbo_net_last_error.restype = C.c_char_p
@@ -58,7 +56,9 @@ def lib():
         L.bbo_net_matmul8_workspace.argtypes = [_I64, _I64, _I64, C.POINTER(_SZ)]
         L.bbo_net_matmul8.argtypes = [_P, _I64, _P, _I64, _I32, _P, _I64, _P, _I64, _I32, _I64, _I64, _I64, _P, _I64, _I32, _I32, _P, _SZ, _P]
         L.bbo_net_adamw.argtypes = [C.POINTER(Tensor), _I32, _I32, _I32, _I32, C.c_double, C.c_double, C.c_double, _I64, _U64, _P, _P]
-        _net = L
+        from . import _net as native  # built with the library
+        native.bind(_check, *(C.cast(getattr(L, name), _P).value for name in EXPORTS[:7]))
+        _net, _ext = L, native
     return _net
 
 
@@ -74,137 +74,38 @@ def _stream(stream, t):
     return _current(t.get_device()) if stream is None else stream.cuda_stream
 
 
-def _room(stream, shape, stride, dtype, device):
-    """A tensor for an output: under the stream that will use it."""
+def _run(name, stream, t, *args):
+    """A function of the extension: on `stream`, or on the current one of t's device."""
+    if _ext is None:
+        lib()
     if stream is None:
-        return _new(shape, stride, dtype=dtype, device=device)
-    with torch.cuda.stream(stream):
-        return _new(shape, stride, dtype=dtype, device=device)
-
-
-def _matrix(t, name, like=None):
-    """A [rows, cols] tensor on the GPU whose rows are dense; of another's type, shape and device."""
-    shape = t.shape
-    if len(shape) != 2 or (t.stride(1) != 1 and shape[1] > 1):
-        raise ValueError("%s must be a [rows, cols] tensor with dense rows" % name)
-    if like is None:
-        if t.dtype not in _DTYPES:
-            raise ValueError("%s must be float32 or bfloat16" % name)
-        if not t.is_cuda:
-            raise ValueError("%s must be on the GPU" % name)
-    elif t.dtype is not like.dtype or shape != like.shape or t.get_device() != like.get_device():
-        raise ValueError("%s must be %s %s on %s" % (name, like.dtype, tuple(like.shape), like.device))
-
-
-def _row(t):
-    """The distance of a matrix's rows: a single row's stride says nothing."""
-    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
-
-
-def _vector(t, name, n, like):
-    if t.dtype is not _FLOAT or t.shape != (n,) or not t.is_contiguous() or t.get_device() != like.get_device():
-        raise ValueError("%s must be a dense float32 [%d] tensor on the same GPU" % (name, n))
+        return getattr(_ext, name)(*args, _current(t.get_device()) if t.is_cuda else 0)
+    with torch.cuda.stream(stream):  # (whose outputs it will use)
+        return getattr(_ext, name)(*args, stream.cuda_stream)
 
 
 def empty_blocks8(rows, cols, tile=1, device="cuda", stream=None):
     """Room for an 8-bit matrix: rows at multiples of 128 bytes, their scales at multiples of 4."""
     kb = (cols + 127) >> 7
-    v = _room(stream, (rows, cols), (kb * BLOCK, 1), _E4M3, device)
-    s = _room(stream, (rows if tile == 1 else (rows + 127) >> 7, kb), ((kb + 3) & ~3, 1), _E8M0, device)
+    with torch.cuda.stream(stream):
+        v = torch.empty_strided((rows, cols), (kb * BLOCK, 1), dtype=torch.float8_e4m3fn, device=device)
+        s = torch.empty_strided((rows if tile == 1 else (rows + 127) >> 7, kb), ((kb + 3) & ~3, 1), dtype=torch.float8_e8m0fnu, device=device)
     return Blocks8(v, s, tile)
-
-
-def _check_blocks(b, name):
-    v, s, tile = b
-    if tile != 1 and tile != BLOCK:
-        raise ValueError("%s: tile must be 1 or 128" % name)
-    shape = v.shape
-    if len(shape) != 2 or v.dtype is not _E4M3 or (v.stride(1) != 1 and shape[1] > 1):
-        raise ValueError("%s: values must be float8_e4m3fn [rows, cols] with dense rows" % name)
-    rows, cols = shape
-    want = (rows if tile == 1 else (rows + 127) >> 7, (cols + 127) >> 7)
-    if s.dtype is not _E8M0 or s.shape != want or (s.stride(1) != 1 and want[1] > 1):
-        raise ValueError("%s: scales must be float8_e8m0fnu %s with dense rows" % (name, want))
-    if not v.is_cuda or s.get_device() != v.get_device():
-        raise ValueError("%s must be on the GPU" % name)
-    return rows, cols
-
-
-@functools.lru_cache(4096)
-def _product_room(m, n, k):
-    need = _SZ(0)
-    _check(lib().bbo_net_matmul8_workspace(m, n, k, C.byref(need)))
-    return need.value
-
-
-@functools.lru_cache(4096)
-def _grad_room(rows, width):
-    need = _SZ(0)
-    _check(lib().bbo_net_rms_norm_grad_workspace(rows, width, C.byref(need)))
-    return max(need.value, 256)
 
 
 def rms_norm(x, weight=None, residual=None, eps=1e-6, want_y=True, want_rstd=False, want_8bit=False, stream=None):
     """h = x + residual (kept as `sum`); y = h / sqrt(mean(h^2) + eps) * weight, per row of x [rows, width].
 
     weight: float32 [width] or None.  y has x's type; y8 is y in 8 bits (tile 1), rounded once.  rstd is for the gradient."""
-    _matrix(x, "x")
-    rows, width = x.shape
-    dtype, device = x.dtype, x.device
-    y = h = rstd = y8 = None
-    pr = pw = ph = py = ps = 0
-    r_stride, q = 0, (0, 0, 0, 0)
-    if residual is not None:
-        _matrix(residual, "residual", x)
-        pr, r_stride = residual.data_ptr(), _row(residual)
-        h = _room(stream, (rows, width), (width, 1), dtype, device)
-        ph = h.data_ptr()
-    if weight is not None:
-        _vector(weight, "weight", width, x)
-        pw = weight.data_ptr()
-    if want_y:
-        y = _room(stream, (rows, width), (width, 1), dtype, device)
-        py = y.data_ptr()
-    if want_rstd:
-        rstd = _room(stream, (rows,), (1,), torch.float32, device)
-        ps = rstd.data_ptr()
-    if want_8bit:
-        y8 = empty_blocks8(rows, width, 1, device, stream)
-        q = (y8.values.data_ptr(), _row(y8.values), y8.scales.data_ptr(), _row(y8.scales))
-    _check((_net or lib()).bbo_net_rms_norm(x.data_ptr(), _row(x), pr, r_stride, pw, rows, width, eps, _DTYPES[dtype], ph, width, py, width, ps, *q,
-                                            _stream(stream, x)))
-    return Norm(y, h, rstd, y8)
+    y, h, rstd, q, s = _run("rms_norm", stream, x, x, weight, residual, eps, want_y, want_rstd, want_8bit)
+    return Norm(y, h, rstd, Blocks8(q, s, 1) if want_8bit else None)
 
 
 def rms_norm_grad(dy, h, rstd, weight=None, dsum=None, want_dweight=True, workspace=None, stream=None):
     """(dx, dweight) of rms_norm: h is its x, or its sum where it had a residual; dsum the gradient that arrives at sum.
 
     dx is the gradient of x and of residual alike; dweight (float32) is None if not wanted."""
-    _matrix(h, "h")
-    rows, width = h.shape
-    dtype, device = h.dtype, h.device
-    _matrix(dy, "dy", h)
-    _vector(rstd, "rstd", rows, h)
-    pd = pw = pg = ws = room = d_stride = 0
-    if dsum is not None:
-        _matrix(dsum, "dsum", h)
-        pd, d_stride = dsum.data_ptr(), _row(dsum)
-    if weight is not None:
-        _vector(weight, "weight", width, h)
-        pw = weight.data_ptr()
-    dx, dw = _room(stream, (rows, width), (width, 1), dtype, device), None
-    L = _net or lib()
-    if want_dweight:
-        dw = _room(stream, (width,), (1,), torch.float32, device)
-        pg = dw.data_ptr()
-        if workspace is None:
-            workspace = _room(stream, (_grad_room(rows, width),), (1,), torch.uint8, device)
-        elif workspace.device != device or not workspace.is_contiguous():
-            raise ValueError("workspace must be dense and on the same GPU")
-        ws, room = workspace.data_ptr(), workspace.numel() * workspace.element_size()
-    _check(L.bbo_net_rms_norm_grad(dy.data_ptr(), _row(dy), pd, d_stride, h.data_ptr(), _row(h), rstd.data_ptr(), pw, rows, width, _DTYPES[dtype],
-                                   dx.data_ptr(), width, pg, ws, room, _stream(stream, h)))
-    return dx, dw
+    return _run("rms_norm_grad", stream, h, dy, h, rstd, weight, dsum, want_dweight, workspace)
 
 
 def quantize(x, tile=1, gate=None, want_rows=True, want_cols=False, stream=None):
@@ -212,54 +113,15 @@ def quantize(x, tile=1, gate=None, want_rows=True, want_cols=False, stream=None)
 
     tile: a scale for 1 x 128 values or for 128 x 128.  gate: like x; values whose gate is <= 0 count as 0 (gate = x is
     ReLU; x a gradient and gate the activation's input is ReLU's gradient)."""
-    _matrix(x, "x")
-    rows, cols = x.shape
-    device = x.device
-    pg = g_stride = 0
-    if gate is not None:
-        _matrix(gate, "gate", x)
-        pg, g_stride = gate.data_ptr(), _row(gate)
-    if tile != 1 and tile != BLOCK:
-        raise ValueError("tile must be 1 or 128")
-    q = empty_blocks8(rows, cols, tile, device, stream) if want_rows else None
-    qt = empty_blocks8(cols, rows, tile, device, stream) if want_cols else None
-    part = lambda b: (b.values.data_ptr(), _row(b.values), b.scales.data_ptr(), _row(b.scales)) if b else (0, 0, 0, 0)
-    _check((_net or lib()).bbo_net_quantize(x.data_ptr(), _row(x), pg, g_stride, rows, cols, _DTYPES[x.dtype], tile, *part(q), *part(qt),
-                                            _stream(stream, x)))
-    return q, qt
+    q, s, qt, st = _run("quantize", stream, x, x, tile, gate, want_rows, want_cols)
+    return Blocks8(q, s, tile) if want_rows else None, Blocks8(qt, st, tile) if want_cols else None
 
 
 def matmul8(a, b, dtype=torch.bfloat16, out=None, accumulate=False, workspace=None, stream=None):
     """a b^T of two Blocks8 [m, k] and [n, k] -> [m, n] in float32 or bfloat16; accumulate adds to `out`."""
-    (m, k), (n, kb) = _check_blocks(a, "a"), _check_blocks(b, "b")
-    av, bv = a.values, b.values
-    on, device = av.get_device(), av.device
-    if kb != k:
-        raise ValueError("a and b must have rows of the same length")
-    if out is None:
-        if accumulate:
-            raise ValueError("accumulate needs an output to add to")
-        if dtype not in _DTYPES:
-            raise ValueError("the output is float32 or bfloat16")
-        out = _room(stream, (m, n), (n, 1), dtype, device)
-    else:
-        _matrix(out, "out")
-        if out.shape != (m, n):
-            raise ValueError("out must have the shape %s" % ((m, n),))
-    if bv.get_device() != on or out.get_device() != on:
-        raise ValueError("all tensors must be on the same GPU")
-    L, ws, room = _net or lib(), 0, 0
-    if workspace is None:
-        need = _product_room(m, n, k)
-        if need:
-            workspace = _room(stream, (need,), (1,), torch.uint8, device)
-    elif workspace.device != device or not workspace.is_contiguous():
-        raise ValueError("workspace must be dense and on the same GPU")
-    if workspace is not None:
-        ws, room = workspace.data_ptr(), workspace.numel() * workspace.element_size()
-    _check(L.bbo_net_matmul8(av.data_ptr(), _row(av), a.scales.data_ptr(), _row(a.scales), a.tile, bv.data_ptr(), _row(bv), b.scales.data_ptr(),
-                             _row(b.scales), b.tile, m, n, k, out.data_ptr(), _row(out), _DTYPES[out.dtype], accumulate, ws, room, _stream(stream, av)))
-    return out
+    if out is None and dtype not in _DTYPES:
+        raise ValueError("the output is float32 or bfloat16")
+    return _run("matmul8", stream, a[0], *a, *b, dtype is torch.float32, out, accumulate, workspace)
 
 
 def _flat(t, name, dtypes, n=None, device=None):
@@ -292,10 +154,7 @@ class AdamW:
         self.moments = [self._zeros(p, stream) for p in self.params] if moments is None else list(moments)
         if not len(self.lr) == len(self.weight_decay) == len(self.moments) == n or (self.copies is not None and len(self.copies) != n):
             raise ValueError("lr, weight_decay, copies and moments must have one entry per parameter")
-        self._table = (Tensor * max(n, 1))()
-        raw = np.frombuffer(self._table, dtype=np.uint64).reshape(-1, C.sizeof(Tensor) // 8)[:n]
-        self._at, self._rates = raw[:, :2], raw[:, 8:9].view(np.float32)  # (p, g) and (lr, weight_decay) of the records
-        self._sizes = [p.numel() for p in self.params]
+        self._table = (Tensor * max(n, 1))()  # (a step fills in the addresses and rates of now)
         for i, p in enumerate(self.params):
             t, k = self._table[i], p.numel()
             t.p, t.n = _flat(p, "parameter", tuple(_DTYPES)), k
@@ -323,24 +182,10 @@ class AdamW:
     def step(self, grads, grad_scale=None, stream=None):
         """One step.  grads: one dense tensor per parameter, float32 or bfloat16 (one type for all); grad_scale: float32
         [1] tensor that multiplies every gradient (clipping), or None."""
-        params, n = self.params, len(self.params)
-        if len(grads) != n:
-            raise ValueError("one gradient per parameter")
-        if not n:
+        if not self.params and not len(grads):
             return
-        dtype, device = grads[0].dtype, params[0].device
-        if dtype not in _DTYPES:
-            raise ValueError("gradients must be float32 or bfloat16")
-        for g, size in zip(grads, self._sizes):
-            if g.dtype is not dtype or g.numel() != size or not g.is_contiguous() or g.device != device:
-                raise ValueError("gradients must be dense, of the parameters' sizes, of one type and on their GPU")
-        self._at[:, 0] = [p.data_ptr() for p in params]
-        self._at[:, 1] = [g.data_ptr() for g in grads]
-        self._rates[:, 0], self._rates[:, 1] = self.lr, self.weight_decay
-        scale = 0
-        if grad_scale is not None:
-            _vector(grad_scale.view(-1), "grad_scale", 1, params[0])
-            scale = grad_scale.data_ptr()
-        _check((_net or lib()).bbo_net_adamw(self._table, n, _DTYPES[params[0].dtype], _DTYPES[dtype], self.eight, self.betas[0], self.betas[1], self.eps,
-                                             self.steps + 1, self.seed, scale, _stream(stream, params[0])))
+        if len(grads) != len(self.params):
+            raise ValueError("one gradient per parameter")
+        _run("adamw", stream, self.params[0], C.addressof(self._table), self.params, grads if type(grads) is list else list(grads), self.lr,
+             self.weight_decay, self.eight, self.betas[0], self.betas[1], self.eps, self.steps + 1, self.seed, grad_scale)
         self.steps += 1
