@@ -203,6 +203,20 @@ def test_rows_of_scales_far_apart(net):
     check(net.matmul8(net.Blocks8(b.values, far.view(torch.float8_e8m0fnu), 1), a, dtype=torch.float32), b, a)
 
 
+@pytest.mark.parametrize("m", [3, 70])
+def test_rows_far_apart(net, m):
+    """Rows of values and of the output at strides past 2^32 bytes."""
+    n, k = 2, 520
+    a, b = matrix(net, m, k, 1, 27), matrix(net, n, k, 1, 28)
+    far = torch.zeros((1 << 32) + 1024, dtype=torch.uint8, device="cuda").as_strided((n, k), ((1 << 32) + 16, 1))
+    far.copy_(b.values.view(torch.uint8))
+    b = net.Blocks8(far.view(torch.float8_e4m3fn), b.scales, 1)
+    check(net.matmul8(a, b, dtype=torch.float32), a, b)
+    out = torch.zeros((1 << 31) + 4096, dtype=torch.bfloat16, device="cuda").as_strided((n, m), ((1 << 31) + 1, 1))
+    check(net.matmul8(b, a, out=out), b, a)
+    check(net.matmul8(b, a, out=out.zero_(), accumulate=True), b, a)
+
+
 def test_the_same_call_gives_the_same_bits(net):
     for m, n, k in ((3, 200, 4000), (100, 100, 4000), (500, 600, 700)):
         a, b = matrix(net, m, k, 1, 13), matrix(net, n, k, 1, 14)
