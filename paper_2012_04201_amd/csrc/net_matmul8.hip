@@ -69,17 +69,20 @@ __device__ inline float scale_of(int byte) {  // 2^(byte - 127), NaN for 255
 // their sum.
 __device__ inline bool in_range(int byte) { return (uint32_t)(byte - 27) <= 200u; }
 
-// 16 bytes of a row from byte `at`, zeros past the row's end.  (Where they do not all belong to the row its last 16 are read and shifted.)
-__device__ inline i32x4 load16(const uint8_t* row, int64_t at, int64_t k) {
+// 16 bytes of a row from byte `at`, zeros past the row's end: read16() and, once they are there, moved16().  (Where they do not all
+// belong to the row its last 16 are read, and moved down; of a row of less than 16 each byte by itself.)
+__device__ inline int64_t from16(int64_t at, int64_t k) { return at + 16 <= k || k < 16 ? at : k - 16; }
+__device__ inline i32x4 read16(const uint8_t* row, int64_t at, int64_t k) {
   if (k < 16) {
     i32x4 v = {0, 0, 0, 0};
     for (int i = 0; at + i < k && i < 16; i++) v[i >> 2] |= (int)row[at + i] << (8 * (i & 3));
     return v;
   }
-  const int64_t from = at + 16 <= k ? at : k - 16;
-  const u32x4_any v = *(const u32x4_any*)(row + from);
-  const int bits = (int)(at - from) * 8;  // 0 .. 128 + 7 * 128
-  uint64_t lo = (uint64_t)v[1] << 32 | v[0], hi = (uint64_t)v[3] << 32 | v[2];
+  return __builtin_bit_cast(i32x4, *(const u32x4_any*)(row + from16(at, k)));
+}
+__device__ inline i32x4 moved16(i32x4 v, int64_t at, int64_t k) {
+  const int bits = (int)(at - from16(at, k)) * 8;  // 0 .. 128 + 7 * 128
+  uint64_t lo = (uint64_t)(uint32_t)v[1] << 32 | (uint32_t)v[0], hi = (uint64_t)(uint32_t)v[3] << 32 | (uint32_t)v[2];
   lo = bits >= 64 ? hi : lo;
   hi = bits >= 64 ? 0 : hi;
   const int rest = bits & 63;
@@ -87,6 +90,7 @@ __device__ inline i32x4 load16(const uint8_t* row, int64_t at, int64_t k) {
   hi >>= rest;
   return i32x4{(int)(uint32_t)lo, (int)(lo >> 32), (int)(uint32_t)hi, (int)(hi >> 32)};
 }
+__device__ inline i32x4 load16(const uint8_t* row, int64_t at, int64_t k) { return moved16(read16(row, at, k), at, k); }
 
 // The part of the contracted index of this workgroup.
 __device__ inline MatArgs my_part(MatArgs g) {
@@ -206,6 +210,83 @@ __device__ inline void block_products(f32x4 (&acc)[MI][NI], const uint32_t (&sa)
       }
     }
   }
+}
+
+// A wave's MI x NI tiles of 16 x 16 from row m, column n on (of its first tile; r16 and q: a lane's place).  Where all are inside, what is to be
+// added to is asked for as a whole, ahead of the stores.
+template <int MI, int NI>
+__device__ inline void put_tiles(const MatArgs& g, int64_t m, int64_t n, int r16, int q, f32x4 (&acc)[MI][NI]) {
+  if (g.splits > 1 || m + MI * 16 > g.m || n + NI * 16 > g.n) {
+#pragma unroll
+    for (int i = 0; i < MI; i++)
+#pragma unroll
+      for (int j = 0; j < NI; j++) put4(g, m + i * 16 + r16, n + j * 16 + q * 4, acc[i][j]);
+    return;
+  }
+  const int64_t first = (m + r16) * g.c_stride + n + q * 4, step = 16 * g.c_stride;
+  // (By so many rows that what is asked for fits beside the sums.)
+  constexpr int AT_ONCE = MI < 4 ? MI : 4;
+  if (g.c_f32) {
+    float* const c = (float*)g.c + first;
+#pragma unroll
+    for (int i0 = 0; i0 < MI; i0 += 2) {
+      u32x4_any o[2][NI];
+      if (g.accumulate) {
+#pragma unroll
+        for (int i = 0; i < 2; i++)
+#pragma unroll
+          for (int j = 0; j < NI; j++) o[i][j] = *(const u32x4_any*)(c + (i0 + i) * step + j * 16);
+#pragma unroll
+        for (int i = 0; i < 2; i++)
+#pragma unroll
+          for (int j = 0; j < NI; j++)
+#pragma unroll
+            for (int k = 0; k < 4; k++) acc[i0 + i][j][k] += as_f32(o[i][j][k]);
+      }
+#pragma unroll
+      for (int i = 0; i < 2; i++)
+#pragma unroll
+        for (int j = 0; j < NI; j++) *(u32x4_any*)(c + (i0 + i) * step + j * 16) = __builtin_bit_cast(u32x4_any, acc[i0 + i][j]);
+    }
+  } else {
+    bf16* const c = (bf16*)g.c + first;
+#pragma unroll
+    for (int i0 = 0; i0 < MI; i0 += AT_ONCE) {
+      if (g.accumulate) {
+        u32x2_any o[AT_ONCE][NI];
+#pragma unroll
+        for (int i = 0; i < AT_ONCE; i++)
+#pragma unroll
+          for (int j = 0; j < NI; j++) o[i][j] = *(const u32x2_any*)(c + (i0 + i) * step + j * 16);
+#pragma unroll
+        for (int i = 0; i < AT_ONCE; i++)
+#pragma unroll
+          for (int j = 0; j < NI; j++)
+#pragma unroll
+            for (int k = 0; k < 4; k++) acc[i0 + i][j][k] += to_f32((bf16)(o[i][j][k >> 1] >> (16 * (k & 1))));
+      }
+#pragma unroll
+      for (int i = 0; i < AT_ONCE; i++)
+#pragma unroll
+        for (int j = 0; j < NI; j++) {
+          const f32x4 v = acc[i0 + i][j];
+          u32x2_any w;
+          w[0] = (uint32_t)from_f32<bf16>(v[0]) | (uint32_t)from_f32<bf16>(v[1]) << 16;
+          w[1] = (uint32_t)from_f32<bf16>(v[2]) | (uint32_t)from_f32<bf16>(v[3]) << 16;
+          *(u32x2_any*)(c + (i0 + i) * step + j * 16) = w;
+        }
+    }
+  }
+}
+
+// A lane's 32 codes of a block, from LDS, without those past the row's end: `here` of them are the row's.
+__device__ inline i32x8 codes_here(i32x8 v, int here) {
+#pragma unroll
+  for (int i = 0; i < 8; i++) {
+    const int bytes = here - 4 * i;
+    v[i] &= bytes >= 4 ? -1 : bytes <= 0 ? 0 : (1 << (8 * bytes)) - 1;
+  }
+  return v;
 }
 
 // Four scales of a row from block kb < blocks on, block kb + i in bits 8 i; 0 past the row's end.
@@ -422,29 +503,35 @@ __global__ __launch_bounds__(64 * WM * WN, WM * WN * PER_CU / 4) void k_mm_tile(
     block(kb, I0);
     if (kb + 1 < direct) block(kb + 1, I1);
   }
+#pragma unroll 1
   for (int kb = direct; kb < blocks; kb++) {
+    i32x4 v[LA + LB];  // (all of them asked for ahead of the first that is waited for)
+#pragma unroll
+    for (int j = 0; j < LA; j++) v[j] = read16(a0 + (int64_t)min((j * W + wave) * 8 + (lane >> 3), rows_a) * g.a_stride, (int64_t)kb * 128 + piece, g.k);
+#pragma unroll
+    for (int j = 0; j < LB; j++) v[LA + j] = read16(b0 + (int64_t)min((j * W + wave) * 8 + (lane >> 3), rows_b) * g.b_stride, (int64_t)kb * 128 + piece, g.k);
     __syncthreads();
-    for (int j = 0; j < LA; j++)
-      *(i32x4*)&lds0[(j * W + wave) * 1024 + lane * 16] =
-          load16(a0 + (int64_t)min((j * W + wave) * 8 + (lane >> 3), rows_a) * g.a_stride, (int64_t)kb * 128 + piece, g.k);
-    for (int j = 0; j < LB; j++)
-      *(i32x4*)&lds0[BM * 128 + (j * W + wave) * 1024 + lane * 16] =
-          load16(b0 + (int64_t)min((j * W + wave) * 8 + (lane >> 3), rows_b) * g.b_stride, (int64_t)kb * 128 + piece, g.k);
+#pragma unroll
+    for (int j = 0; j < LA + LB; j++) *(i32x4*)&lds0[(j * W + wave) * 1024 + lane * 16] = moved16(v[j], (int64_t)kb * 128 + piece, g.k);
     next_scales(kb);
     __syncthreads();
     products(kb, I0);
   }
+  if constexpr (EXACT) {  // (put_tiles() here takes registers from the loop: 8192^3 922 -> 960 us)
 #pragma unroll
-  for (int i = 0; i < MI; i++)
+    for (int i = 0; i < MI; i++)
 #pragma unroll
-    for (int j = 0; j < NI; j++) put4(g, m0 + wm + i * 16 + r16, n0 + wn + j * 16 + q * 4, acc[i][j]);
+      for (int j = 0; j < NI; j++) put4(g, m0 + wm + i * 16 + r16, n0 + wn + j * 16 + q * 4, acc[i][j]);
+  } else {
+    put_tiles<MI, NI>(g, m0 + wm, n0 + wn, r16, q, acc);
+  }
 }
 
 // ---------------------------------------------------------------------------
 // Tiles of 64 x 64 by 2 x 2 waves, where there are few: bound by the way of a block to LDS, so that three are on it while one is
-// multiplied: 200 x 4096 x 4096 to bfloat16 12 us (one on its way: 20).  A last part of a block, and rows at other addresses, are asked
-// for ahead into registers: 1797 x 1000 x 569 to float32 11.4 us (asked for when they are due: 16); five blocks there are a chain of a
-// launch, the first rows' way (6.5 us in all for 64 x 64 x 128), 0.75 us a block and the part's.
+// multiplied: 200 x 4096 x 4096 to bfloat16 12 us (one on its way: 20).  Of a last part of a block those pieces of 16 bytes that hold a byte
+// of the row go to LDS like the others: 1797 x 1000 x 569 10.6 us to float32 and 7.5 to bfloat16 (through registers, asked for when they
+// are due, 16 and 13); five blocks there are a chain of a launch, the first rows' way (6.5 us in all for 64 x 64 x 128) and 0.75 us a block.
 // ---------------------------------------------------------------------------
 // All waves' loads but their last VM have landed, all their reads from LDS but the last LGKM are done.
 template <int VM, int LGKM>
@@ -485,23 +572,26 @@ __global__ __launch_bounds__(256, 2) void k_mm_small(const MatArgs whole, int ti
   for (int j = 0; j < LA; j++) from_a[j] = (uint32_t)min(lane_row + j * W * 8, rows_a) * (uint32_t)g.a_stride + piece;
 #pragma unroll
   for (int j = 0; j < LB; j++) from_b[j] = (uint32_t)min(lane_row + j * W * 8, rows_b) * (uint32_t)g.b_stride + piece;
-  auto stage = [&](auto at, int kb) {  // (past the last block: nothing reads it; a wait counts the loads behind its own)
-    const int k = min(kb, direct - 1) * 128;
+  const int staged = g.direct ? blocks : 0;
+  auto stage = [&](auto at, int kb) {  // (past the last block: nothing reads it; a wait counts the loads behind its own; 
+  // of a last part of a block those pieces that hold a byte of the row, as a whole: 16 bytes at a multiple of 16, which lie where that byte
+  // does; the first stands for the others, and products() leaves out what is past the end)
+    const int k = min(kb, staged - 1) * 128, back = k + (int64_t)piece >= g.k ? piece : 0;
 #pragma unroll
     for (int j = 0; j < LA; j++)
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(buf_a, (__attribute__((address_space(3))) void*)(lds(at) + (j * W + wave) * 1024), 16, from_a[j], k, 0, 0);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(buf_a, (__attribute__((address_space(3))) void*)(lds(at) + (j * W + wave) * 1024), 16, from_a[j] - back, k, 0, 0);
 #pragma unroll
     for (int j = 0; j < LB; j++)
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(buf_b, (__attribute__((address_space(3))) void*)(lds(at) + BM * 128 + (j * W + wave) * 1024), 16, from_b[j], k, 0, 0);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(buf_b, (__attribute__((address_space(3))) void*)(lds(at) + BM * 128 + (j * W + wave) * 1024), 16, from_b[j] - back, k, 0, 0);
   };
-  i32x4 rest[LA + LB];  // of a block that does not go by itself
+  i32x4 rest[LA + LB];  // of rows that do not go by themselves
   auto ask_rest = [&](int kb) {
 #pragma unroll
-    for (int j = 0; j < LA; j++) rest[j] = load16(a0 + (int64_t)min(lane_row + j * W * 8, rows_a) * g.a_stride, (int64_t)kb * 128 + piece, g.k);
+    for (int j = 0; j < LA; j++) rest[j] = read16(a0 + (int64_t)min(lane_row + j * W * 8, rows_a) * g.a_stride, (int64_t)kb * 128 + piece, g.k);
 #pragma unroll
-    for (int j = 0; j < LB; j++) rest[LA + j] = load16(b0 + (int64_t)min(lane_row + j * W * 8, rows_b) * g.b_stride, (int64_t)kb * 128 + piece, g.k);
+    for (int j = 0; j < LB; j++) rest[LA + j] = read16(b0 + (int64_t)min(lane_row + j * W * 8, rows_b) * g.b_stride, (int64_t)kb * 128 + piece, g.k);
   };
-  if (direct < blocks) ask_rest(direct);
+  if (staged < blocks) ask_rest(0);
   // Scales: those of four blocks of a lane's rows, in four bytes.
   const uint8_t* const as = g.as + (m0 >> g.a_shift) * g.as_stride;
   const uint8_t* const bs = g.bs + (n0 >> g.b_shift) * g.bs_stride;
@@ -510,13 +600,14 @@ __global__ __launch_bounds__(256, 2) void k_mm_small(const MatArgs whole, int ti
   uint32_t sa[MI], sb[NI];
   f32x4 acc[MI][NI] = {};
   const int place = r16 * 128 + (q * 2 ^ mix(r16)) * 16;  // a lane's place in 16 rows; its second 16 bytes are at place ^ 16
-  auto products = [&](auto at, auto u) {
+  auto products = [&](const uint8_t* in, auto u, int here) __attribute__((always_inline)) {
     auto codes = [&](const uint8_t* from) {
       const i32x4 lo = *(const i32x4*)(from + place), hi = *(const i32x4*)(from + (place ^ 16));
-      return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+      const i32x8 v = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+      return here < 32 ? codes_here(v, here) : v;
     };
-    block_products<EXACT, u, false, MI, NI>(acc, sa, sb, [&](int i) { return codes(lds(at) + (wm + i * 16) * 128); },
-                                            [&](int j) { return codes(lds(at) + (BM + wn + j * 16) * 128); });
+    block_products<EXACT, u, false, MI, NI>(acc, sa, sb, [&](int i) { return codes(in + (wm + i * 16) * 128); },
+                                            [&](int j) { return codes(in + (BM + wn + j * 16) * 128); });
   };
   // (64-bit offsets: rows of scales may be as far apart as they like)
   uint32_t next_a[MI], next_b[NI];
@@ -546,7 +637,7 @@ __global__ __launch_bounds__(256, 2) void k_mm_small(const MatArgs whole, int ti
       for (int i = 0; i < NI; i++) next_b[i] = *(const u32_any*)(bs + at + off_b[i]);
     }
   };
-  if (direct > 0) {
+  if (staged > 0) {
     stage(Int<0>{}, 0);
     stage(Int<1>{}, 1);
     stage(Int<2>{}, 2);
@@ -554,7 +645,7 @@ __global__ __launch_bounds__(256, 2) void k_mm_small(const MatArgs whole, int ti
       all_here<2 * (LA + LB), 0>();  // this block has landed, and what the last one read is free
       if constexpr (u == 0) next_scales(kb);
       stage(Int<u + 3>{}, kb + 3);
-      products(u, u);
+      products(lds(u), u, 32);
     };
     int kb = 0;
 #pragma unroll 1
@@ -585,17 +676,18 @@ __global__ __launch_bounds__(256, 2) void k_mm_small(const MatArgs whole, int ti
 #pragma unroll
       for (int i = 0; i < NI; i++) sb[i] >>= 8;
     }
+    if (!g.direct) {
 #pragma unroll
-    for (int j = 0; j < LA + LB; j++) *(i32x4*)&lds0[(j * W + wave) * 1024 + lane * 16] = rest[j];
-    __syncthreads();
-    if (kb + 1 < blocks) ask_rest(kb + 1);
-    products(Int<0>{}, Int<0>{});
+      for (int j = 0; j < LA + LB; j++) *(i32x4*)&lds0[(j * W + wave) * 1024 + lane * 16] = moved16(rest[j], (int64_t)kb * 128 + piece, g.k);
+      __syncthreads();
+      if (kb + 1 < blocks) ask_rest(kb + 1);
+    }
+    const int64_t left = g.k - kb * 128ll - q * 32;
+    const uint8_t* const in = (direct & 3) == 0 ? lds0 : (direct & 3) == 1 ? lds1 : (direct & 3) == 2 ? lds2 : lds3;
+    products(in, Int<0>{}, left < 0 ? 0 : left > 32 ? 32 : (int)left);
     __syncthreads();
   }
-#pragma unroll
-  for (int i = 0; i < MI; i++)
-#pragma unroll
-    for (int j = 0; j < NI; j++) put4(g, m0 + wm + i * 16 + r16, n0 + wn + j * 16 + q * 4, acc[i][j]);
+  put_tiles<MI, NI>(g, m0 + wm, n0 + wn, r16, q, acc);
 #endif
 }
 
@@ -803,13 +895,19 @@ __global__ __launch_bounds__(512, 2) void k_mm_pipe(const MatArgs g, int tiles_m
   }
   for (int kb = direct; kb < blocks; kb++) {  // the last part of a block
     __syncthreads();
-    auto part = [&](const uint8_t* row, uint8_t* to) { *(i32x4*)(to + wave * 1024 + lane * 16) = load16(row, (int64_t)kb * 128 + piece16, g.k); };
-    auto part_a = [&](auto p) { part(a0 + (int64_t)min(lane_row + row_a + p * 32, rows_a) * g.a_stride, quarter_of(p, I0)); };
-    part_a(I0);
-    part_a(I1);
-    part_a(I2);
-    part_a(I3);
-    for (int j = 0; j < 4; j++) part(b0 + (int64_t)min(lane_row + row_b + j * 64, rows_b) * g.b_stride, first0 + B_AT + j * 8192);
+    i32x4 v[8];  // (all of them asked for ahead of the first that is waited for)
+#pragma unroll
+    for (int j = 0; j < 4; j++) {
+      v[j] = read16(a0 + (int64_t)min(lane_row + row_a + j * 32, rows_a) * g.a_stride, (int64_t)kb * 128 + piece16, g.k);
+      v[4 + j] = read16(b0 + (int64_t)min(lane_row + row_b + j * 64, rows_b) * g.b_stride, (int64_t)kb * 128 + piece16, g.k);
+    }
+    auto part = [&](i32x4 x, uint8_t* to) { *(i32x4*)(to + wave * 1024 + lane * 16) = moved16(x, (int64_t)kb * 128 + piece16, g.k); };
+    part(v[0], quarter_of(I0, I0));
+    part(v[1], quarter_of(I1, I0));
+    part(v[2], quarter_of(I2, I0));
+    part(v[3], quarter_of(I3, I0));
+#pragma unroll
+    for (int j = 0; j < 4; j++) part(v[4 + j], first0 + B_AT + j * 8192);
     if ((kb & 3) == 0) keep_scales(kb & 4, load_scales(scales + srow, kb, blocks));
     all_here<0, 0>();
     read_b(I0, I0);
@@ -825,10 +923,7 @@ __global__ __launch_bounds__(512, 2) void k_mm_pipe(const MatArgs g, int tiles_m
     all(I2);
     all(I3);
   }
-#pragma unroll
-  for (int i = 0; i < 8; i++)
-#pragma unroll
-    for (int j = 0; j < 4; j++) put4(g, m0 + wm * 128 + i * 16 + r16, n0 + wn * 64 + j * 16 + q * 4, acc[i][j]);
+  put_tiles<8, 4>(g, m0 + wm * 128, n0 + wn * 64, r16, q, acc);
 #endif
 }
 

@@ -83,6 +83,18 @@ def test_many_tiles(net, m, n, k):
     check(net.matmul8(a, b, dtype=torch.float32), a, b)
 
 
+@pytest.mark.parametrize("m,n,k", [(3300, 2001, 300), (1000, 3100, 1024), (700, 900, 333), (64, 128, 1), (128, 256, 130), (4352, 4096, 600)])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_added_to_inside_and_at_the_edges(net, m, n, k, dtype):
+    """Tiles that are inside are added to as a whole, those at an edge value by value; rows of c at any address, and what is beside c untouched."""
+    a, b = matrix(net, m, k, 1, 29), matrix(net, n, k, 128, 30)
+    wide = (torch.randn(m, n + 3, generator=torch.Generator().manual_seed(31)) * 10).to(dtype).cuda()
+    c0, sides = wide[:, 1:1 + n].clone(), (wide[:, :1].clone(), wide[:, 1 + n:].clone())
+    net.matmul8(a, b, out=wide[:, 1:1 + n], accumulate=True)
+    check(wide[:, 1:1 + n], a, b, c0)
+    assert torch.equal(wide[:, :1], sides[0]) and torch.equal(wide[:, 1 + n:], sides[1])
+
+
 @pytest.mark.parametrize("m,n,k", [(3300, 4000, 385), (3333, 3845, 512), (3400, 3840, 640), (3585, 3601, 900), (3300, 4000, 1024), (6200, 1900, 1151), (4500, 4000, 641),
                                    (4110, 4097, 512), (17000, 1000, 1000)])
 def test_many_large_tiles(net, m, n, k):
