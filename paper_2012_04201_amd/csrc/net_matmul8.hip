@@ -61,10 +61,6 @@ __device__ inline f32x4 mfma16(const Wide& b, const Wide& a, f32x4 c) {
   for (int i = 0; i < 4; i++) c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b.v[i], a.v[i], c, 0, 0, 0);
   return c;
 }
-__device__ inline float scale_of(int byte) {  // 2^(byte - 127), NaN for 255
-  const uint32_t b = (uint32_t)byte;
-  return as_f32(b == 255 ? 0x7fc00000u : b == 0 ? 0x00400000u : b << 23);
-}
 // Scales that go into bfloat16 operands: with others an operand would leave that type's range, and the block's products are scaled after
 // their sum.
 __device__ inline bool in_range(int byte) { return (uint32_t)(byte - 27) <= 200u; }
@@ -200,12 +196,15 @@ __device__ inline void block_products(f32x4 (&acc)[MI][NI], const uint32_t (&sa)
 #pragma unroll
       for (int i = 0; i < MI; i++) {
         const Wide a = widen(get_a(i), 1.f);
-        const float s = scale_of(byte(sa[i]));
+        const int e = byte(sa[i]);
 #pragma unroll
         for (int j = 0; j < NI; j++) {
           const f32x4 t = mfma16(b[j], a, f32x4{0.f, 0.f, 0.f, 0.f});
 #pragma unroll
-          for (int r = 0; r < 4; r++) acc[i][j][r] += t[r] * (s * scale_of(__shfl(byte(sb[j]), q4 + r)));
+          for (int r = 0; r < 4; r++) {  // (by the exponents' sum: the scales' product may be out of range where the product is not)
+            const int f = __shfl(byte(sb[j]), q4 + r);
+            acc[i][j][r] += e == 255 || f == 255 ? __builtin_nanf("") : __builtin_ldexpf(t[r], e + f - 254);
+          }
         }
       }
     }

@@ -122,6 +122,20 @@ def test_scales_from_one_end_to_the_other(net, m):
     assert torch.equal(got.isnan(), nan)
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("m", [1, 40, 200])
+def test_zeros_under_the_largest_scales(net, m, dtype):
+    """Blocks of zeros add nothing, whatever their scales; scales far apart from each other meet in a product that is in range."""
+    n, k = 96, 640
+    a, b = matrix(net, m, k, 1, 32), matrix(net, n, k, 1, 33)
+    for block, ea, eb in ((0, 254, 254), (2, 0, 254), (3, 250, 3), (4, 254, 0)):
+        a.scales.view(torch.uint8)[:, block], b.scales.view(torch.uint8)[:, block] = ea, eb
+    a.values.view(torch.uint8)[:, :128] = 0
+    check(net.matmul8(a, b, dtype=dtype), a, b)
+    b.values.view(torch.uint8)[:, :128] = 0
+    check(net.matmul8(a, b, dtype=dtype), a, b)
+
+
 def test_nothing_contracted(net):
     a, b = net.empty_blocks8(5, 0), net.empty_blocks8(70, 0)
     assert (net.matmul8(a, b) == 0).all()
